@@ -399,6 +399,60 @@ int kvs_decode_attn(const void* q, const void* k_cache, const void* v_cache,
                     float softmax_scale, int num_splits, void* out, float* lse,
                     void* workspace, size_t workspace_bytes, kvs_stream_t stream);
 
+/*
+ * Eviction by accumulated attention weight.  token_weight: fp32 [num_seqs, max_pages * page_size], the weight that every live token
+ * has drawn so far, in the order of the live cache (kvs_decode_attn_weights adds to it), 0 behind the last live token.
+ * Sequences with more than `budget` live tokens lose whole pages until they have no more than that: candidates are the full pages
+ * that hold none of the first keep_first and none of the last keep_recent live tokens; the score of a page is the sum of its tokens'
+ * weights (added in 64 bits, rounded to 32; a NaN counts as more than any number), the lowest scores leave, of equal ones the earlier
+ * pages; where there are too few candidates all of them leave.  The pages that stay keep their order, token_weight moves with them,
+ * the tokens that left have weight 0 behind the last one, n_tokens drops, and the pages go back on the stack in a fixed order.
+ * evicted: int32 [num_seqs, max_pages], the table slots (before the call) that left, ascending, then -1; may be NULL.  What left is
+ * what the trainer's evict_at needs: the caller knows which tokens the slots held.  n_evicted: int32 [num_seqs], pages.
+ * n_tokens of a sequence that its table cannot hold: KVS_ERR_INVALID_ARG in the cache status word, that sequence stays as it is.
+ * A sequence's weights, table and scores have to fit into the shared memory of a cluster: about 160000 tokens with pages of one token,
+ * 380000 with pages of 16; larger max_pages * page_size return KVS_ERR_UNSUPPORTED.
+ * kvs_cache_evict does not know of token_weight: a cache with weights is not evicted by ranges.
+ */
+int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recent,
+                           int num_seqs, int page_size, int max_pages, int num_pages,
+                           int32_t* block_table, int32_t* n_tokens, int32_t* free_list,
+                           float* token_weight, int32_t* evicted, int32_t* n_evicted, kvs_stream_t stream);
+/*
+ * Appends n_new tokens (k_new, v_new: bf16 [num_seqs, n_new, Hkv, head_dim]) to every sequence whose `active` byte is non-zero
+ * (active == NULL: all), in order.  All of them or none: where the free pages or a table do not suffice nothing changes and the cache
+ * status is KVS_ERR_WORKSPACE (KVS_ERR_INVALID_ARG for lengths or a stack that make no sense).  Pages are taken in the order of the sequences.
+ */
+int kvs_cache_append_tokens(const void* k_new, const void* v_new, const uint8_t* active,
+                            int num_seqs, int n_new, int Hkv, int head_dim, int page_size, int max_pages, int num_pages,
+                            int32_t* block_table, int32_t* n_tokens, int32_t* free_list,
+                            void* k_cache, void* v_cache, kvs_stream_t stream);
+/*
+ * Drops the last n_drafted - n_accepted[s] live tokens of every sequence (n_accepted: int32 [num_seqs]): what is left of a round of
+ * drafted tokens after verification.  Pages without a live token go back on the stack, in the order that undoes
+ * kvs_cache_append_tokens.  token_weight (may be NULL): the dropped tokens' weights become 0.  A sequence whose count is negative, above
+ * n_drafted, or asks for more tokens than are live stays as it is and sets KVS_ERR_INVALID_ARG in the cache status word.
+ */
+int kvs_cache_truncate(int n_drafted, const int32_t* n_accepted,
+                       int num_seqs, int page_size, int max_pages, int num_pages,
+                       const int32_t* block_table, int32_t* n_tokens, int32_t* free_list,
+                       float* token_weight, kvs_stream_t stream);
+/*
+ * Verification of drafted tokens against the target's probabilities, from given random numbers in [0, 1): the tokens that result are
+ * distributed as if the target had generated them.
+ *   target_probs fp32 [num_seqs, n_draft + 1, vocab], draft_probs fp32 [num_seqs, n_draft, vocab], draft_tokens int32 [num_seqs, n_draft],
+ *   u_accept fp32 [num_seqs, n_draft], u_sample fp32 [num_seqs]
+ * Draft i (token x) is accepted while u_accept_i * draft_i(x) < target_i(x); the first that is not ends it, and the next token is drawn
+ * from w = max(target_r - draft_r, 0) (the target's row itself where that is 0 everywhere); with all accepted w = target_n.  Drawn: the
+ * least k with w_0 + .. + w_k > u_sample * sum w.  Products, differences and sums in 64 bits.  Rows need not add up to 1.
+ *   tokens int32 [num_seqs, n_draft + 1]: the accepted drafts, the drawn token, then -1;  n_accepted int32 [num_seqs]
+ * A drafted token outside [0, vocab) is not accepted; NaN and negative weights count as 0; a row without weight gives token -1.
+ * vocab <= 2^24, n_draft <= 65535 (0: only a draw).
+ */
+int kvs_verify_drafts(const float* target_probs, const float* draft_probs, const int32_t* draft_tokens,
+                      const float* u_accept, const float* u_sample, int num_seqs, int n_draft, int vocab,
+                      int32_t* tokens, int32_t* n_accepted, kvs_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -68,6 +68,10 @@ SIGNATURES = {
     "kvs_decode_num_splits": (_i, [_i, _i, _i]),
     "kvs_decode_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "kvs_decode_attn": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _f, _i, _vp, _vp, _vp, _sz, _vp]),
+    "kvs_cache_evict_lowest": (_i, [_i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "kvs_cache_append_tokens": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "kvs_cache_truncate": (_i, [_i, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp]),
+    "kvs_verify_drafts": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp]),
     "kvs_host_arena_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
     "kvs_attn_fwd_bwd_host": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _f, _i,
                                    _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -373,6 +377,32 @@ def kvs_attn_fwd_bwd_host(evict_at, cu_seqlens, q, k, v, dout, max_seqlen: int, 
 # ------------------------------------------------------------------------------------------
 # rollout side: paged KV cache with physical eviction, decode attention
 # ------------------------------------------------------------------------------------------
+def kvs_cache_append_tokens(k_new, v_new, block_table, n_tokens, free_list, k_cache, v_cache, active=None, stream=None) -> None:
+    """Appends k_new, v_new [num_seqs, n_new, Hkv, d] bf16 to every (active) sequence: all tokens of the call or none."""
+    _calls().cache_append_tokens(k_new, v_new, active, block_table, n_tokens, free_list, k_cache, v_cache, stream)
+
+
+def kvs_cache_truncate(n_drafted: int, n_accepted, page_size: int, block_table, n_tokens, free_list, token_weight=None, stream=None) -> None:
+    """Sequence s loses its last n_drafted - n_accepted[s] live tokens (n_accepted int32 [num_seqs])."""
+    _calls().cache_truncate(n_drafted, n_accepted, page_size, block_table, n_tokens, free_list, token_weight, stream)
+
+
+def kvs_cache_evict_lowest(budget: int, keep_first: int, keep_recent: int, page_size: int, block_table, n_tokens, free_list, token_weight,
+                           evicted=None, n_evicted=None, stream=None):
+    """The pages with the lowest accumulated weight leave every sequence of more than `budget` live tokens.  token_weight fp32
+    [num_seqs, max_pages * page_size].  Returns (evicted int32 [num_seqs, max_pages], the slots that left, then -1; n_evicted
+    int32 [num_seqs])."""
+    return _calls().cache_evict_lowest(budget, keep_first, keep_recent, page_size, block_table, n_tokens, free_list, token_weight, evicted,
+                                       n_evicted, stream)
+
+
+def kvs_verify_drafts(target_probs, draft_probs, draft_tokens, u_accept, u_sample, tokens=None, n_accepted=None, stream=None):
+    """target_probs fp32 [num_seqs, n + 1, vocab], draft_probs fp32 [num_seqs, n, vocab], draft_tokens int32 [num_seqs, n], u_accept
+    fp32 [num_seqs, n], u_sample fp32 [num_seqs].  Returns (tokens int32 [num_seqs, n + 1]: the accepted drafts, the token drawn
+    after them, then -1; n_accepted int32 [num_seqs])."""
+    return _calls().verify_drafts(target_probs, draft_probs, draft_tokens, u_accept, u_sample, tokens, n_accepted, stream)
+
+
 class PagedCache:
     """Device buffers of a paged KV cache plus the calls that maintain it.  Holds no logic:
     every operation is one call into the library."""

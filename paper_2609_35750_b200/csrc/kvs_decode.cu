@@ -17,7 +17,7 @@
 //                          because with a wide GQA group the CUDA-core kernel is bound by its
 //                          arithmetic, not by the bytes, and because TMA keeps more bytes in flight
 //                          than the load/store unit can.
-#include "kvs_common.cuh"
+#include "kvs_cache.cuh"
 #include <cstring>
 
 namespace kvs {
@@ -722,12 +722,6 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 }
 
 // ---- cache maintenance ---------------------------------------------------------------------------
-struct CacheHeader {            // the first 16 bytes of the free-list buffer
-    int32_t top;                // number of free pages on the stack
-    int32_t status;             // KVS_OK or an error recorded by a kernel
-    int32_t pad[2];
-};
-
 __global__ void cache_init_kernel(int32_t* free_buf, int num_pages) {
     CacheHeader* hdr = reinterpret_cast<CacheHeader*>(free_buf);
     int32_t* stack = free_buf + 4;

@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/Exceptions.h>
@@ -20,7 +21,7 @@ namespace {
 #define KVS_FUNCTIONS(X) \
     X(kvs_mask_meta_bytes) X(kvs_mask_meta) X(kvs_mask_meta_keys) X(kvs_mask_meta_evicted) X(kvs_attn_fwd) X(kvs_attn_fwd_packed) \
     X(kvs_attn_fwd_dual) X(kvs_attn_bwd) X(kvs_attn_bwd_packed) X(kvs_attn_bwd_workspace_bytes) X(kvs_permute_rows) X(kvs_rope_qk) \
-    X(kvs_cache_append) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
+    X(kvs_cache_append) X(kvs_cache_append_tokens) X(kvs_cache_truncate) X(kvs_cache_evict_lowest) X(kvs_verify_drafts) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
 #define KVS_POINTER(name) decltype(&::name) name = nullptr;
 struct Library {
     KVS_FUNCTIONS(KVS_POINTER)
@@ -378,6 +379,119 @@ PyObject* decode(PyObject* const* a) {
     return tuple({wrap(out, a[3]), wrap(lse, a[4])});
 }
 
+// ---- bounded caches and drafted tokens ------------------------------------------------------------------------------
+// These calls work on the device of their first tensor, whichever is current, and allocate on the stream they are given: the
+// allocator then hands the memory out again in that stream's order.
+struct On {
+    c10::cuda::CUDAGuard device;
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    kvs_stream_t stream;
+    On(const at::Tensor& t, const char* name, PyObject* o) : device(on_gpu(t, name)) {
+        if (given(o)) {
+            stream = stream_of(o);
+            guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)stream, t.get_device()));
+        } else {
+            stream = (kvs_stream_t)c10::cuda::getCurrentCUDAStream(t.get_device()).stream();
+        }
+    }
+    static c10::Device on_gpu(const at::Tensor& t, const char* name) {
+        if (!t.is_cuda()) value_error("%s must be a CUDA tensor (there is no CPU path)", name);
+        return t.device();
+    }
+};
+// address of a contiguous tensor of these sizes (-1: any) on that device
+void* checked(const at::Tensor& t, const char* name, at::ScalarType dtype, std::initializer_list<int64_t> sizes, const at::Tensor& like) {
+    void* p = address(t, name, dtype);
+    bool same = t.dim() == (int64_t)sizes.size();
+    int64_t i = 0;
+    for (int64_t n : sizes) same = same && (n < 0 || t.size(i) == n), ++i;
+    if (!same) value_error("%s has the wrong shape", name);
+    if (t.device() != like.device()) value_error("%s is on another device", name);
+    return p;
+}
+// a size that the C interface takes as an int
+int small(int64_t n, const char* name) {
+    if (n > 0x7fffffff) value_error("%s is too large", name);
+    return (int)n;
+}
+
+// (k_new, v_new, active, block_table, n_tokens, free_list, k_cache, v_cache, stream)
+PyObject* cache_append_tokens(PyObject* const* a) {
+    const at::Tensor &k = tensor(a[0], "k_new"), &v = tensor(a[1], "v_new"), &table = tensor(a[3], "block_table"), &n = tensor(a[4], "n_tokens"),
+                     &free = tensor(a[5], "free_list"), &kc = tensor(a[6], "k_cache"), &vc = tensor(a[7], "v_cache");
+    dims(k, 4, "k_new");
+    dims(kc, 4, "k_cache");
+    dims(table, 2, "block_table");
+    const int64_t S = k.size(0), Hkv = k.size(2), d = k.size(3), pages = kc.size(0), page = kc.size(1);
+    const On on(k, "k_new", a[8]);
+    const void *pk = checked(k, "k_new", BF16, {S, -1, Hkv, d}, k), *pv = checked(v, "v_new", BF16, {S, k.size(1), Hkv, d}, k);
+    const uint8_t* active = given(a[2]) ? (const uint8_t*)checked(tensor(a[2], "active"), "active", U8, {S}, k) : nullptr;
+    int32_t *pt = (int32_t*)checked(table, "block_table", I32, {S, -1}, k), *pn = (int32_t*)checked(n, "n_tokens", I32, {S}, k),
+            *pf = (int32_t*)checked(free, "free_list", I32, {4 + pages}, k);
+    void *pkc = checked(kc, "k_cache", BF16, {-1, -1, Hkv, d}, k), *pvc = checked(vc, "v_cache", BF16, {pages, page, Hkv, d}, k);
+    const int i[] = {small(S, "k_new"), small(k.size(1), "k_new"), small(Hkv, "k_new"), small(d, "k_new"), small(page, "k_cache"),
+                     small(table.size(1), "block_table"), small(pages, "k_cache")};
+    call("kvs_cache_append_tokens", [&] {
+        return lib.kvs_cache_append_tokens(pk, pv, active, i[0], i[1], i[2], i[3], i[4], i[5], i[6], pt, pn, pf, pkc, pvc, on.stream);
+    });
+    Py_RETURN_NONE;
+}
+
+// (n_drafted, n_accepted, page_size, block_table, n_tokens, free_list, token_weight, stream)
+PyObject* cache_truncate(PyObject* const* a) {
+    const int drafted = whole(a[0]), page = whole(a[2]);
+    const at::Tensor &acc = tensor(a[1], "n_accepted"), &table = tensor(a[3], "block_table"), &n = tensor(a[4], "n_tokens"), &free = tensor(a[5], "free_list");
+    dims(table, 2, "block_table");
+    dims(free, 1, "free_list");
+    const int64_t S = table.size(0), P = table.size(1);
+    const On on(table, "block_table", a[7]);
+    const int32_t* pt = (const int32_t*)checked(table, "block_table", I32, {S, P}, table);
+    const int32_t* pa = (const int32_t*)checked(acc, "n_accepted", I32, {S}, table);
+    int32_t *pn = (int32_t*)checked(n, "n_tokens", I32, {S}, table), *pf = (int32_t*)checked(free, "free_list", I32, {-1}, table);
+    float* pw = given(a[6]) ? (float*)checked(tensor(a[6], "token_weight"), "token_weight", F32, {S, P * (int64_t)page}, table) : nullptr;
+    const int i[] = {small(S, "block_table"), small(P, "block_table"), small(free.size(0) - 4, "free_list")};
+    call("kvs_cache_truncate", [&] { return lib.kvs_cache_truncate(drafted, pa, i[0], page, i[1], i[2], pt, pn, pf, pw, on.stream); });
+    Py_RETURN_NONE;
+}
+
+// (budget, keep_first, keep_recent, page_size, block_table, n_tokens, free_list, token_weight, evicted, n_evicted, stream)
+PyObject* cache_evict_lowest(PyObject* const* a) {
+    const int budget = whole(a[0]), first = whole(a[1]), recent = whole(a[2]), page = whole(a[3]);
+    const at::Tensor &table = tensor(a[4], "block_table"), &n = tensor(a[5], "n_tokens"), &free = tensor(a[6], "free_list"), &w = tensor(a[7], "token_weight");
+    dims(table, 2, "block_table");
+    dims(free, 1, "free_list");
+    const int64_t S = table.size(0), P = table.size(1);
+    const On on(table, "block_table", a[10]);
+    int32_t* pt = (int32_t*)checked(table, "block_table", I32, {S, P}, table);
+    int32_t *pn = (int32_t*)checked(n, "n_tokens", I32, {S}, table), *pf = (int32_t*)checked(free, "free_list", I32, {-1}, table);
+    float* pw = (float*)checked(w, "token_weight", F32, {S, P * (int64_t)page}, table);
+    const at::Tensor evicted = out_of(a[8], "evicted", {S, P}, table, I32), count = out_of(a[9], "n_evicted", {S}, table, I32);
+    int32_t *pe = (int32_t*)checked(evicted, "evicted", I32, {S, P}, table), *pc = (int32_t*)checked(count, "n_evicted", I32, {S}, table);
+    const int i[] = {small(S, "block_table"), small(P, "block_table"), small(free.size(0) - 4, "free_list")};
+    call("kvs_cache_evict_lowest", [&] {
+        return lib.kvs_cache_evict_lowest(budget, first, recent, i[0], page, i[1], i[2], pt, pn, pf, pw, pe, pc, on.stream);
+    });
+    return tuple({wrap(evicted, a[8]), wrap(count, a[9])});
+}
+
+// (target_probs, draft_probs, draft_tokens, u_accept, u_sample, tokens, n_accepted, stream)
+PyObject* verify_drafts(PyObject* const* a) {
+    const at::Tensor &p = tensor(a[0], "target_probs"), &q = tensor(a[1], "draft_probs"), &x = tensor(a[2], "draft_tokens"), &ua = tensor(a[3], "u_accept"),
+                     &us = tensor(a[4], "u_sample");
+    dims(p, 3, "target_probs");
+    dims(q, 3, "draft_probs");
+    const int64_t S = q.size(0), drafts = q.size(1), V = p.size(2);
+    const On on(p, "target_probs", a[7]);
+    const float *pp = (const float*)checked(p, "target_probs", F32, {S, drafts + 1, V}, p), *pq = (const float*)checked(q, "draft_probs", F32, {S, drafts, V}, p);
+    const int32_t* px = (const int32_t*)checked(x, "draft_tokens", I32, {S, drafts}, p);
+    const float *pua = (const float*)checked(ua, "u_accept", F32, {S, drafts}, p), *pus = (const float*)checked(us, "u_sample", F32, {S}, p);
+    const at::Tensor tokens = out_of(a[5], "tokens", {S, drafts + 1}, p, I32), count = out_of(a[6], "n_accepted", {S}, p, I32);
+    int32_t *pt = (int32_t*)checked(tokens, "tokens", I32, {S, drafts + 1}, p), *pc = (int32_t*)checked(count, "n_accepted", I32, {S}, p);
+    const int i[] = {small(S, "target_probs"), small(drafts, "draft_probs"), small(V, "target_probs")};
+    call("kvs_verify_drafts", [&] { return lib.kvs_verify_drafts(pp, pq, px, pua, pus, i[0], i[1], i[2], pt, pc, on.stream); });
+    return tuple({wrap(tokens, a[5]), wrap(count, a[6])});
+}
+
 // ---- the module ---------------------------------------------------------------------------------------------------
 // A call's C++ errors (torch's among them) become Python errors, as torch's own functions have them.
 template <PyObject* (*F)(PyObject* const*), int N>
@@ -436,6 +550,10 @@ PyMethodDef methods[] = {
     KVS_ENTRY(rope_qk, 9),
     KVS_ENTRY(cache_append, 15),
     KVS_ENTRY(decode, 16),
+    KVS_ENTRY(cache_append_tokens, 9),
+    KVS_ENTRY(cache_truncate, 8),
+    KVS_ENTRY(cache_evict_lowest, 11),
+    KVS_ENTRY(verify_drafts, 8),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvs_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
