@@ -400,6 +400,36 @@ int kvs_decode_attn(const void* q, const void* k_cache, const void* v_cache,
                     void* workspace, size_t workspace_bytes, kvs_stream_t stream);
 
 /*
+ * Attention of the last n_new live tokens of every sequence (one, or several drafted ones; their K and V rows are in the cache) with a
+ * sliding window and a few first tokens that stay visible.  With n live tokens query t of n_new stands at p = n - n_new + t and sees
+ * live token j iff  j <= p  and  (j < sinks or j > p - window):  window >= 1 tokens with the query's own, 2^31-1 for all; sinks >= 0.
+ * Distances are counted in live tokens.
+ *   out[s,t,h] = softmax_j(scale * q[s,t,h].k_j) v_j, lse[s,t,h] = log sum_j exp(scale * q.k_j)
+ * q, out: bf16 [num_seqs, n_new, Hq, head_dim]; lse: fp32 [num_seqs, n_new, Hq].  Hq/Hkv <= 64.  A query that sees nothing (a sequence
+ * with fewer live tokens than n_new) gets out = 0, lse = -inf.  Keys that a query does not see do not reach its result, whatever they hold.
+ * num_splits: kvs_decode_window_num_splits gives one that fills the GPU.  workspace: >= kvs_decode_workspace_bytes(num_seqs * n_new, Hq,
+ * head_dim, num_splits), 256-byte aligned.  Everything else as in kvs_decode_attn.
+ */
+int kvs_decode_window_num_splits(int num_seqs, int n_new, int Hq, int Hkv, int max_tokens, int window, int sinks);
+int kvs_decode_attn_window(const void* q, const void* k_cache, const void* v_cache,
+                           const int32_t* block_table, const int32_t* n_tokens,
+                           int num_seqs, int n_new, int Hq, int Hkv, int head_dim, int page_size, int max_pages, int num_pages,
+                           float softmax_scale, int window, int sinks, int num_splits, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, kvs_stream_t stream);
+/*
+ * kvs_decode_attn that also accumulates attention weights: token_weight[s, j] += sum over query heads h of
+ * exp(scale * q[s,h].k_j - lse[s,h]) for every live token j (fp32 [num_seqs, max_pages * page_size], in the order of the live
+ * cache, as kvs_cache_evict_lowest takes it), the heads added in order.  max_tokens: no sequence has more live tokens; the workspace has
+ * room for that many scores per query head.  A longer sequence gets its attention, keeps its weights, and sets KVS_ERR_INVALID_ARG in
+ * the workspace's status word.  Hq <= 8192.  Everything else as in kvs_decode_attn.
+ */
+size_t kvs_decode_weights_workspace_bytes(int num_seqs, int Hq, int head_dim, int num_splits, int max_tokens);
+int kvs_decode_attn_weights(const void* q, const void* k_cache, const void* v_cache,
+                            const int32_t* block_table, const int32_t* n_tokens,
+                            int num_seqs, int Hq, int Hkv, int head_dim, int page_size, int max_pages, int num_pages,
+                            float softmax_scale, int num_splits, int max_tokens, void* out, float* lse, float* token_weight,
+                            void* workspace, size_t workspace_bytes, kvs_stream_t stream);
+/*
  * Eviction by accumulated attention weight.  token_weight: fp32 [num_seqs, max_pages * page_size], the weight that every live token
  * has drawn so far, in the order of the live cache (kvs_decode_attn_weights adds to it), 0 behind the last live token.
  * Sequences with more than `budget` live tokens lose whole pages until they have no more than that: candidates are the full pages

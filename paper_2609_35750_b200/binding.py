@@ -68,6 +68,10 @@ SIGNATURES = {
     "kvs_decode_num_splits": (_i, [_i, _i, _i]),
     "kvs_decode_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "kvs_decode_attn": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _f, _i, _vp, _vp, _vp, _sz, _vp]),
+    "kvs_decode_window_num_splits": (_i, [_i, _i, _i, _i, _i, _i, _i]),
+    "kvs_decode_attn_window": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _f, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "kvs_decode_weights_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "kvs_decode_attn_weights": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _f, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "kvs_cache_evict_lowest": (_i, [_i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "kvs_cache_append_tokens": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
     "kvs_cache_truncate": (_i, [_i, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp]),
@@ -377,6 +381,24 @@ def kvs_attn_fwd_bwd_host(evict_at, cu_seqlens, q, k, v, dout, max_seqlen: int, 
 # ------------------------------------------------------------------------------------------
 # rollout side: paged KV cache with physical eviction, decode attention
 # ------------------------------------------------------------------------------------------
+def kvs_decode_attn_window(q, k_cache, v_cache, block_table, n_tokens, window: int, sinks: int = 0, softmax_scale: float = 0.0,
+                           num_splits: int = 0, out=None, lse=None, workspace=None, max_tokens: Optional[int] = None, stream=None):
+    """Attention of the last n_new live tokens, q bf16 [num_seqs, n_new, Hq, d], each over the `window` live tokens up to its own and the
+    first `sinks`.  max_tokens: live tokens of the longest sequence, for the choice of splits (default: what a table can hold).
+    Returns (out bf16 [num_seqs, n_new, Hq, d], lse fp32 [num_seqs, n_new, Hq])."""
+    return _calls().decode_window(q, k_cache, v_cache, block_table, n_tokens, window, sinks, softmax_scale, num_splits, out, lse, workspace,
+                                  max_tokens or 0, stream)
+
+
+def kvs_decode_attn_weights(q, k_cache, v_cache, block_table, n_tokens, token_weight, softmax_scale: float = 0.0, num_splits: int = 0, out=None,
+                            lse=None, workspace=None, max_tokens: Optional[int] = None, stream=None):
+    """Decode attention of q bf16 [num_seqs, Hq, d] over the live cache; token_weight fp32 [num_seqs, max_pages * page_size] grows by
+    every live token's softmax weight, summed over the query heads.  max_tokens: no sequence is longer (default: what a table can
+    hold).  Returns (out bf16 [num_seqs, Hq, d], lse fp32 [num_seqs, Hq])."""
+    return _calls().decode_weights(q, k_cache, v_cache, block_table, n_tokens, token_weight, softmax_scale, num_splits, out, lse, workspace,
+                                   max_tokens or 0, stream)
+
+
 def kvs_cache_append_tokens(k_new, v_new, block_table, n_tokens, free_list, k_cache, v_cache, active=None, stream=None) -> None:
     """Appends k_new, v_new [num_seqs, n_new, Hkv, d] bf16 to every (active) sequence: all tokens of the call or none."""
     _calls().cache_append_tokens(k_new, v_new, active, block_table, n_tokens, free_list, k_cache, v_cache, stream)
@@ -407,7 +429,8 @@ class PagedCache:
     """Device buffers of a paged KV cache plus the calls that maintain it.  Holds no logic:
     every operation is one call into the library."""
 
-    def __init__(self, num_pages: int, page_size: int, num_seqs: int, max_pages: int, Hkv: int, head_dim: int, device="cuda"):
+    def __init__(self, num_pages: int, page_size: int, num_seqs: int, max_pages: int, Hkv: int, head_dim: int, device="cuda",
+                 track_weights: bool = False):
         self.num_pages, self.page_size, self.num_seqs, self.max_pages = num_pages, page_size, num_seqs, max_pages
         self.Hkv, self.d = Hkv, head_dim
         self.k_cache = torch.zeros((num_pages, page_size, Hkv, head_dim), dtype=torch.bfloat16, device=device)
@@ -415,6 +438,8 @@ class PagedCache:
         self.block_table = torch.zeros((num_seqs, max_pages), dtype=torch.int32, device=device)
         self.n_tokens = torch.zeros(num_seqs, dtype=torch.int32, device=device)
         self.free_list = torch.zeros(int(load().kvs_cache_free_list_bytes(num_pages)) // 4, dtype=torch.int32, device=device)
+        # accumulated attention weight of every live token (decode_weights, evict_lowest)
+        self.token_weight = torch.zeros((num_seqs, max_pages * page_size), dtype=torch.float32, device=device) if track_weights else None
         _check(load().kvs_cache_init(self.free_list.data_ptr(), num_pages, _stream(None)), "kvs_cache_init")
 
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, active: Optional[torch.Tensor] = None, stream=None) -> None:
@@ -423,6 +448,8 @@ class PagedCache:
 
     def evict(self, ranges: torch.Tensor, stream=None) -> None:
         """ranges int32 [n, 3] rows (sequence, first_page_slot, n_pages) (device)."""
+        if self.token_weight is not None:
+            raise ValueError("a cache that tracks weights is evicted by evict_lowest: ranges would leave the weights behind")
         n = ranges.shape[0] if ranges.numel() else 0
         _check(load().kvs_cache_evict(_dev(ranges, "ranges", torch.int32) if n else None, n, self.num_seqs, self.page_size,
                                       self.max_pages, self.num_pages, self.block_table.data_ptr(), self.n_tokens.data_ptr(),
@@ -439,3 +466,33 @@ class PagedCache:
         """q bf16 [num_seqs, Hq, d] -> (out bf16 [num_seqs, Hq, d], lse fp32 [num_seqs, Hq])."""
         return _calls().decode(q, softmax_scale, num_splits, out, lse, workspace, max_tokens or self.max_pages * self.page_size, self.Hkv,
                                self.page_size, self.max_pages, self.num_pages, self.block_table, self.n_tokens, self.k_cache, self.v_cache, stream)
+
+    def append_tokens(self, k_new: torch.Tensor, v_new: torch.Tensor, active: Optional[torch.Tensor] = None, stream=None) -> None:
+        """k_new, v_new bf16 [num_seqs, n_new, Hkv, d]: all tokens of the call, or none."""
+        kvs_cache_append_tokens(k_new, v_new, self.block_table, self.n_tokens, self.free_list, self.k_cache, self.v_cache, active, stream)
+
+    def truncate(self, n_drafted: int, n_accepted: torch.Tensor, stream=None) -> None:
+        """Sequence s loses its last n_drafted - n_accepted[s] tokens."""
+        kvs_cache_truncate(n_drafted, n_accepted, self.page_size, self.block_table, self.n_tokens, self.free_list, self.token_weight, stream)
+
+    def decode_window(self, q: torch.Tensor, window: int, sinks: int = 0, softmax_scale: float = 0.0, num_splits: int = 0, out=None, lse=None,
+                      workspace=None, max_tokens: Optional[int] = None, stream=None):
+        """q bf16 [num_seqs, n_new, Hq, d], the last n_new live tokens -> (out, lse fp32 [num_seqs, n_new, Hq])."""
+        return kvs_decode_attn_window(q, self.k_cache, self.v_cache, self.block_table, self.n_tokens, window, sinks, softmax_scale, num_splits, out, lse,
+                                      workspace, max_tokens, stream)
+
+    def _tracked(self) -> torch.Tensor:
+        if self.token_weight is None:
+            raise ValueError("the cache was made without track_weights")
+        return self.token_weight
+
+    def decode_weights(self, q: torch.Tensor, softmax_scale: float = 0.0, num_splits: int = 0, out=None, lse=None, workspace=None,
+                       max_tokens: Optional[int] = None, stream=None):
+        """decode, and every live token's weight joins token_weight."""
+        return kvs_decode_attn_weights(q, self.k_cache, self.v_cache, self.block_table, self.n_tokens, self._tracked(), softmax_scale, num_splits, out, lse,
+                                       workspace, max_tokens, stream)
+
+    def evict_lowest(self, budget: int, keep_first: int = 0, keep_recent: int = 1, evicted=None, n_evicted=None, stream=None):
+        """The pages with the lowest accumulated weight leave sequences of more than `budget` tokens -> (evicted, n_evicted)."""
+        return kvs_cache_evict_lowest(budget, keep_first, keep_recent, self.page_size, self.block_table, self.n_tokens, self.free_list, self._tracked(),
+                                      evicted, n_evicted, stream)

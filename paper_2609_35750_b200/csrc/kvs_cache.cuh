@@ -12,6 +12,20 @@ struct CacheHeader {            // the first 16 bytes of the free-list buffer
     int32_t pad;
 };
 
+constexpr size_t DEC_WS_HEADER = 256;       // of a decode workspace: {magic, status}; the splits' results follow
+
+// The splits of (sequence, token, query head) rows and where their merged results go
+struct MergeParams {
+    const float* part_o;
+    const float* part_ml;
+    __nv_bfloat16* out;
+    float* lse;
+    int32_t* header;
+    int rows, nsplit;
+};
+// the merge of a decode call, in kvs_decode.cu
+int launch_decode_merge(const MergeParams& m, int head_dim, cudaStream_t st);
+
 #ifdef __CUDACC__
 // launch_after with clusters of `cluster` CTAs along x
 template <typename... P, typename... A>
@@ -31,6 +45,27 @@ inline int launch_clusters_after(void (*kernel)(P...), dim3 grid, int cluster, i
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess ? KVS_OK : cuda_refused();
+}
+
+// The status of a call is gathered with its partial results, so that no launch of its own has to reset the workspace's word before
+// any CTA may write to it: a CTA that met an error (a bad page id, a wait that ran out) hands over its sums, which are never
+// negative, with the sign bit set and the kind in the lowest bit.  The first CTA writes {magic, OK}, the merge adds the errors.
+__device__ __forceinline__ float flagged_sum(float sum, int status) {
+    const uint32_t bits = __float_as_uint(sum) & 0x7fffffffu;
+    return __uint_as_float(status == KVS_OK ? bits : (bits & ~1u) | 0x80000000u | (status == KVS_ERR_TIMEOUT ? 1u : 0u));
+}
+__device__ __forceinline__ float sum_and_status(float flagged, int32_t* status) {
+    const uint32_t bits = __float_as_uint(flagged);
+    if (bits >> 31) set_status(status, bits & 1u ? KVS_ERR_TIMEOUT : KVS_ERR_INVALID_ARG);
+    return __uint_as_float(bits & 0x7fffffffu);
+}
+// TMA gather: the 64-column slice starting at column c0 of the four rows r0..r3 of a 2-D tensor lands in four
+// consecutive 128-byte rows at dst (swizzled by address like a tiled box); completes 512 bytes on the barrier.
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, int c0, int r0, int r1, int r2, int r3, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar)
+        : "memory");
 }
 
 // Sum of `v` over the CTA's threads before this one (a whole number of warps, 32 at most); `total`: over all of them.  s_warp: 33 entries.

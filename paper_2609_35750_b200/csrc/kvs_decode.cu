@@ -23,7 +23,6 @@
 namespace kvs {
 
 constexpr int DEC_THREADS = 128;
-constexpr size_t DEC_WS_HEADER = 256;
 
 struct DecodeParams {
     const __nv_bfloat16* q;          // [S, Hq, D]
@@ -38,20 +37,10 @@ struct DecodeParams {
     float scale_log2;
     float* part_o;                   // [S, Hq, nsplit, D] unnormalised
     float* part_ml;                  // [S, Hq, nsplit, 2]  (max in base-2 units, sum; see flagged_sum)
+    float* scores;                   // kvs_decode_attn_weights: [S, Hq, score_stride] scores in base-2 units of the live tokens
+    int score_stride;                // most tokens of a sequence, in whole tiles
 };
 
-// The status of a call is gathered with its partial results, so that no launch of its own has to reset the workspace's word before
-// any CTA may write to it: a CTA that met an error (a bad page id, a wait that ran out) hands over its sums, which are never
-// negative, with the sign bit set and the kind in the lowest bit.  The first CTA writes {magic, OK}, the merge adds the errors.
-__device__ __forceinline__ float flagged_sum(float sum, int status) {
-    const uint32_t bits = __float_as_uint(sum) & 0x7fffffffu;
-    return __uint_as_float(status == KVS_OK ? bits : (bits & ~1u) | 0x80000000u | (status == KVS_ERR_TIMEOUT ? 1u : 0u));
-}
-__device__ __forceinline__ float sum_and_status(float flagged, int32_t* status) {
-    const uint32_t bits = __float_as_uint(flagged);
-    if (bits >> 31) set_status(status, bits & 1u ? KVS_ERR_TIMEOUT : KVS_ERR_INVALID_ARG);
-    return __uint_as_float(bits & 0x7fffffffu);
-}
 __device__ __forceinline__ void decode_header(const DecodeParams& p) {
     if ((blockIdx.x | blockIdx.y | blockIdx.z | threadIdx.x) == 0) {
         p.header[0] = (int32_t)WS_MAGIC;
@@ -66,14 +55,7 @@ __device__ __forceinline__ void decode_header(const DecodeParams& p) {
 // finish, with counts in the workspace, cost every CTA a fence and an atomic and the merge its parallelism (a step in a CUDA
 // graph, merge in the last CTA -> here, us: 1 x 24000 tokens with 8 heads on 1 29.6 -> 15.0, 1 x 2000 with 32 on 8 14.2 -> 12.7,
 // 100 x 300 with 8 on 8 and head_dim 64 17.4 -> 13.5; launched call by call 30.4 -> 15.8, 14.6 -> 13.3, 17.9 -> 13.8).
-struct MergeParams {
-    const float* part_o;
-    const float* part_ml;
-    __nv_bfloat16* out;
-    float* lse;
-    int32_t* header;
-    int rows, nsplit;
-};
+// (MergeParams: kvs_cache.cuh)
 template <int D, int PART>
 __device__ __forceinline__ void decode_merge_row(const MergeParams& p, size_t row, int lane) {
     constexpr int PER = D / 32;
@@ -131,6 +113,57 @@ __global__ void __launch_bounds__(256) decode_merge_kernel(MergeParams p) {
     if (row < p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31);
 }
 
+// kvs_decode_attn_weights: token_weight[s, j] += sum over query heads of exp2(score - lse), the heads in order, so that the sums do
+// not depend on which CTA comes first.  In the same launch as the merge: its CTAs come first, the others have a sequence and WT_TOKENS
+// tokens each and form the sequence's lse from the splits themselves.  The scores (4 bytes a token and query head) were written by
+// the kernels that formed them and are read once: forming them again would take the K rows (256 bytes a token and KV head).
+constexpr int WT_PER = 4, WT_TOKENS = 256 * WT_PER;
+struct WeightParams {
+    const float* scores;
+    const int32_t* n_tokens;
+    float* weight;                   // [S, weight_stride]
+    int Hq, score_stride, merge_ctas, chunks;
+    int weight_stride;               // max_pages * page_size: no sequence has more tokens
+};
+template <int D, int PART>
+__global__ void __launch_bounds__(256) decode_merge_weights_kernel(MergeParams p, WeightParams w) {
+    extern __shared__ float s_lse[];                     // [Hq] in base-2 units
+    pdl_wait();
+    if ((int)blockIdx.x < w.merge_ctas) {
+        const int row = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+        if (row < p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31);
+        return;
+    }
+    const int s = (blockIdx.x - w.merge_ctas) / w.chunks, j0 = (blockIdx.x - w.merge_ctas - s * w.chunks) * WT_TOKENS + threadIdx.x;
+    const int n = min(max(w.n_tokens[s], 0), w.weight_stride);
+    if (n > w.score_stride || j0 - (int)threadIdx.x >= n) return;            // the same in the whole CTA
+    for (int h = threadIdx.x; h < w.Hq; h += blockDim.x) {
+        const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)s * w.Hq + h) * p.nsplit;
+        float M = -INFINITY, L = 0.f;
+        for (int z = 0; z < p.nsplit; ++z) M = fmaxf(M, __ldcg(ml + z).x);
+        for (int z = 0; z < p.nsplit; ++z) {
+            const float2 x = __ldcg(ml + z);
+            L += fabsf(x.y) * fast_exp2(x.x - M);                            // the sign says that the split met an error: the merge tells
+        }
+        s_lse[h] = M + log2f(L);
+    }
+    __syncthreads();
+    float* weight = w.weight + (size_t)s * w.weight_stride;
+    const float* sc = w.scores + (size_t)s * w.Hq * w.score_stride;
+    float sum[WT_PER] = {}, old[WT_PER];
+#pragma unroll
+    for (int i = 0; i < WT_PER; ++i) old[i] = j0 + i * 256 < n ? weight[j0 + i * 256] : 0.f;
+#pragma unroll 4
+    for (int h = 0; h < w.Hq; ++h) {
+#pragma unroll
+        for (int i = 0; i < WT_PER; ++i)
+            if (j0 + i * 256 < n) sum[i] += fast_exp2(__ldcg(sc + (size_t)h * w.score_stride + j0 + i * 256) - s_lse[h]);
+    }
+#pragma unroll
+    for (int i = 0; i < WT_PER; ++i)
+        if (j0 + i * 256 < n) weight[j0 + i * 256] = old[i] + sum[i];
+}
+
 // A block-table entry is only followed if it names a page of the cache: anything else (a stale or
 // corrupt table) is recorded as KVS_ERR_INVALID_ARG and read as page 0, so no kernel reads outside the cache.
 // token index -> (entry of the block table, row inside the page) without a division for power-of-two pages
@@ -145,6 +178,13 @@ __device__ __forceinline__ void split_token(const DecodeParams& p, int tok, int&
 }
 __device__ __forceinline__ int checked_page(const DecodeParams& p, int page) {
     if ((unsigned)page < (unsigned)p.num_pages) return page;
+    set_status(p.status, KVS_ERR_INVALID_ARG);
+    return 0;
+}
+
+// Tokens whose scores are written: all, or none of a sequence that is longer than the caller said (there is no room for them)
+__device__ __forceinline__ int scored_tokens(const DecodeParams& p, int n) {
+    if (n <= p.score_stride) return n;
     set_status(p.status, KVS_ERR_INVALID_ARG);
     return 0;
 }
@@ -171,7 +211,7 @@ struct RowChunk {
     }
 };
 
-template <int D, int G>
+template <int D, int G, bool SCORES>
 __global__ void __launch_bounds__(DEC_THREADS, (G > 4) ? 2 : 3)
 decode_partial_kernel(DecodeParams p) {
     constexpr int CH = D / 16;                  // elements of a row per lane (16 lanes per row): 8 or 4
@@ -188,6 +228,7 @@ decode_partial_kernel(DecodeParams p) {
     const int half = lane >> 4, l16 = lane & 15;
     const int n = min(max(p.n_tokens[s], 0), p.max_pages * p.page_size);    // never past the sequence's table
     const int ps = p.page_size;
+    const int n_scores = SCORES ? scored_tokens(p, n) : 0;
     const int nblocks = (n + BLK - 1) / BLK;
     // blocks of this split, dealt round-robin to (split, warp)
     const int stride = p.nsplit * (DEC_THREADS / 32);
@@ -264,6 +305,8 @@ decode_partial_kernel(DecodeParams p) {
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);      // within the 16 lanes of the row
                 sc[r][h] = ok ? v : -INFINITY;
+                if (SCORES && l16 == h && t0 + 2 * r + half < n_scores)
+                    p.scores[((size_t)s * p.Hq + g * G + h) * p.score_stride + t0 + 2 * r + half] = v;
             }
         }
         // one softmax update per head for the ROWS tokens of this half-warp
@@ -381,16 +424,7 @@ __device__ __forceinline__ int float_order(float x) {
 }
 __device__ __forceinline__ float float_unorder(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 
-// TMA gather: the 64-column slice starting at column c0 of the four rows r0..r3 of a 2-D tensor lands in four
-// consecutive 128-byte rows at dst (swizzled by address like a tiled box); completes 512 bytes on the barrier.
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, int c0, int r0, int r1, int r2, int r3, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-        ::"r"(dst), "l"(map), "r"(c0), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar)
-        : "memory");
-}
-
-template <int G, int LOAD>
+template <int G, int LOAD, bool SCORES>
 __global__ void __launch_bounds__(DTC_THREADS, 3)
 decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, DecodeParams p) {
     constexpr int D = 128;
@@ -582,6 +616,7 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             }
         };
         const __nv_bfloat16* v_lane = p.v_cache + (size_t)g * D + (lane & 15) * 8;       // this lane's 16 bytes of a row of head g
+        const int n_scores = SCORES ? scored_tokens(p, n) : 0;
         const int v_row_elems = p.Hkv * D;
         auto load_v_rows = [&](int tt) {
             const int nvalid = min(128, n - tt * 128);
@@ -617,6 +652,7 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
             for (int h = 0; h < G; ++h) {
                 sc[h] = (tid < nvalid) ? __uint_as_float(r[h]) * p.scale_log2 : -INFINITY;
+                if (SCORES && tt * 128 + tid < n_scores) p.scores[((size_t)s * p.Hq + g * G + h) * p.score_stride + tt * 128 + tid] = sc[h];
                 const int wm = __reduce_max_sync(0xffffffffu, float_order(sc[h]));
                 if (lane == 0) wmax[warp * 16 + h] = float_unorder(wm);
             }
@@ -965,16 +1001,16 @@ extern "C" size_t kvs_decode_workspace_bytes(int num_seqs, int Hq, int head_dim,
     return DEC_WS_HEADER + align_up(sizeof(float) * (size_t)num_seqs * Hq * num_splits * (head_dim + 2), 256);
 }
 
-template <int G, int LOAD>
+template <int G, int LOAD, bool SCORES>
 static int launch_decode_tc(const CUtensorMap& tk, const CUtensorMap& tv, const DecodeParams& p, cudaStream_t st) {
-    auto kern = decode_tc_kernel<G, LOAD>;
+    auto kern = decode_tc_kernel<G, LOAD, SCORES>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, DtcSmem::DYN_BYTES) != cudaSuccess) return cuda_refused();
     dim3 grid(p.nsplit, p.Hkv, p.S);
     return launch_after(kern, grid, DTC_THREADS, DtcSmem::DYN_BYTES, st, tk, tv, p);
 }
 
-template <int D>
-static int launch_decode(const DecodeParams& p, int G, const void* k_cache, const void* v_cache, __nv_bfloat16* out, float* lse, cudaStream_t st) {
+template <int D, bool SCORES>
+static int launch_partials(const DecodeParams& p, int G, const void* k_cache, const void* v_cache, cudaStream_t st) {
     dim3 grid(p.nsplit, p.Hkv, p.S);
     const int ps = p.page_size;
     // tensor-core variant (head_dim 128).  Pages that are whole 8-row swizzle atoms and tile 128 tokens exactly come in
@@ -996,11 +1032,11 @@ static int launch_decode(const DecodeParams& p, int G, const void* k_cache, cons
             if ((rc = make_tmap_thd(&tk, k_cache, p.num_pages * ps, p.Hkv, 128, ps)) != KVS_OK) return rc;
             if ((rc = make_tmap_thd(&tv, v_cache, p.num_pages * ps, p.Hkv, 128, ps)) != KVS_OK) return rc;
             switch (G) {
-                case 1: rc = launch_decode_tc<1, DTC_PAGES>(tk, tv, p, st); break;
-                case 2: rc = launch_decode_tc<2, DTC_PAGES>(tk, tv, p, st); break;
-                case 4: rc = launch_decode_tc<4, DTC_PAGES>(tk, tv, p, st); break;
-                case 7: rc = launch_decode_tc<7, DTC_PAGES>(tk, tv, p, st); break;
-                default: rc = launch_decode_tc<8, DTC_PAGES>(tk, tv, p, st); break;
+                case 1: rc = launch_decode_tc<1, DTC_PAGES, SCORES>(tk, tv, p, st); break;
+                case 2: rc = launch_decode_tc<2, DTC_PAGES, SCORES>(tk, tv, p, st); break;
+                case 4: rc = launch_decode_tc<4, DTC_PAGES, SCORES>(tk, tv, p, st); break;
+                case 7: rc = launch_decode_tc<7, DTC_PAGES, SCORES>(tk, tv, p, st); break;
+                default: rc = launch_decode_tc<8, DTC_PAGES, SCORES>(tk, tv, p, st); break;
             }
         } else {
             // the K cache as (Hkv * d, rows): a gather names four rows and a 64-column slice of one KV head (V is
@@ -1008,33 +1044,63 @@ static int launch_decode(const DecodeParams& p, int G, const void* k_cache, cons
             if ((long long)p.num_pages * ps > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
             if ((rc = make_tmap_rows(&tk, k_cache, p.num_pages * ps, p.Hkv * 128)) != KVS_OK) return rc;
             switch (G) {
-                case 1: rc = launch_decode_tc<1, DTC_ROWS>(tk, tv, p, st); break;
-                case 2: rc = launch_decode_tc<2, DTC_ROWS>(tk, tv, p, st); break;
-                case 4: rc = launch_decode_tc<4, DTC_ROWS>(tk, tv, p, st); break;
-                case 7: rc = launch_decode_tc<7, DTC_ROWS>(tk, tv, p, st); break;
-                default: rc = launch_decode_tc<8, DTC_ROWS>(tk, tv, p, st); break;
+                case 1: rc = launch_decode_tc<1, DTC_ROWS, SCORES>(tk, tv, p, st); break;
+                case 2: rc = launch_decode_tc<2, DTC_ROWS, SCORES>(tk, tv, p, st); break;
+                case 4: rc = launch_decode_tc<4, DTC_ROWS, SCORES>(tk, tv, p, st); break;
+                case 7: rc = launch_decode_tc<7, DTC_ROWS, SCORES>(tk, tv, p, st); break;
+                default: rc = launch_decode_tc<8, DTC_ROWS, SCORES>(tk, tv, p, st); break;
             }
         }
         if (rc != KVS_OK) return rc;
     } else {
         int rc = KVS_ERR_UNSUPPORTED;
         switch (G) {
-            case 1: rc = launch_after(decode_partial_kernel<D, 1>, grid, DEC_THREADS, 0, st, p); break;
-            case 2: rc = launch_after(decode_partial_kernel<D, 2>, grid, DEC_THREADS, 0, st, p); break;
-            case 4: rc = launch_after(decode_partial_kernel<D, 4>, grid, DEC_THREADS, 0, st, p); break;
-            case 7: rc = launch_after(decode_partial_kernel<D, 7>, grid, DEC_THREADS, 0, st, p); break;
-            case 8: rc = launch_after(decode_partial_kernel<D, 8>, grid, DEC_THREADS, 0, st, p); break;
+            case 1: rc = launch_after(decode_partial_kernel<D, 1, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+            case 2: rc = launch_after(decode_partial_kernel<D, 2, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+            case 4: rc = launch_after(decode_partial_kernel<D, 4, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+            case 7: rc = launch_after(decode_partial_kernel<D, 7, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+            case 8: rc = launch_after(decode_partial_kernel<D, 8, SCORES>, grid, DEC_THREADS, 0, st, p); break;
         }
         if (rc != KVS_OK) return rc;
     }
-    const MergeParams m = {p.part_o, p.part_ml, out, lse, p.header, p.S * p.Hq, p.nsplit};
-    return launch_after(p.nsplit <= 4 ? decode_merge_kernel<D, 4> : decode_merge_kernel<D, 16>, (m.rows + 7) / 8, 256, 0, st, m);
+    return KVS_OK;
 }
 
-extern "C" int kvs_decode_attn(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
-                               const int32_t* n_tokens, int num_seqs, int Hq, int Hkv, int head_dim, int page_size, int max_pages,
-                               int num_pages, float softmax_scale, int num_splits, void* out, float* lse, void* workspace, size_t workspace_bytes,
-                               kvs_stream_t stream) {
+namespace kvs {
+int launch_decode_merge(const MergeParams& m, int head_dim, cudaStream_t st) {
+    const int ctas = (m.rows + 7) / 8;
+    if (head_dim == 64) return launch_after(m.nsplit <= 4 ? decode_merge_kernel<64, 4> : decode_merge_kernel<64, 16>, ctas, 256, 0, st, m);
+    return launch_after(m.nsplit <= 4 ? decode_merge_kernel<128, 4> : decode_merge_kernel<128, 16>, ctas, 256, 0, st, m);
+}
+}  // namespace kvs
+
+template <int D>
+static int launch_decode(const DecodeParams& p, int G, const void* k_cache, const void* v_cache, __nv_bfloat16* out, float* lse, float* weight, cudaStream_t st) {
+    const int rc = weight ? launch_partials<D, true>(p, G, k_cache, v_cache, st) : launch_partials<D, false>(p, G, k_cache, v_cache, st);
+    if (rc != KVS_OK) return rc;
+    const MergeParams m = {p.part_o, p.part_ml, out, lse, p.header, p.S * p.Hq, p.nsplit};
+    const int merge_ctas = (m.rows + 7) / 8;
+    if (!weight) return launch_decode_merge(m, D, st);
+    const int most = min(p.score_stride, p.max_pages * p.page_size), chunks = (most + WT_TOKENS - 1) / WT_TOKENS;
+    const WeightParams w = {p.scores, p.n_tokens, weight, p.Hq, p.score_stride, merge_ctas, chunks, p.max_pages * p.page_size};
+    if ((long long)merge_ctas + (long long)p.S * chunks > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
+    return launch_after(p.nsplit <= 4 ? decode_merge_weights_kernel<D, 4> : decode_merge_weights_kernel<D, 16>, merge_ctas + p.S * chunks, 256,
+                        sizeof(float) * (size_t)p.Hq, st, m, w);
+}
+
+// Scores of a call with weights: rows of whole tiles, so that a tile's scores start on a 512-byte line
+static size_t score_bytes(int num_seqs, int Hq, int max_tokens) { return sizeof(float) * (size_t)num_seqs * Hq * align_up((size_t)max_tokens, 128); }
+
+extern "C" size_t kvs_decode_weights_workspace_bytes(int num_seqs, int Hq, int head_dim, int num_splits, int max_tokens) {
+    const size_t n = kvs_decode_workspace_bytes(num_seqs, Hq, head_dim, num_splits);
+    if (n == 0 || max_tokens <= 0 || max_tokens > 0x7fffff00) return 0;
+    return n + score_bytes(num_seqs, Hq, max_tokens);
+}
+
+// max_tokens: of a call with weights, else 0
+static int decode_call(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table, const int32_t* n_tokens, int num_seqs, int Hq,
+                       int Hkv, int head_dim, int page_size, int max_pages, int num_pages, float softmax_scale, int num_splits, int max_tokens, void* out,
+                       float* lse, float* token_weight, void* workspace, size_t workspace_bytes, kvs_stream_t stream) {
     if (num_seqs < 0 || Hq <= 0 || Hkv <= 0 || page_size <= 0 || max_pages <= 0 || num_pages <= 0 || num_splits <= 0)
         return KVS_ERR_INVALID_ARG;
     if (head_dim != 64 && head_dim != 128) return KVS_ERR_UNSUPPORTED;
@@ -1043,7 +1109,8 @@ extern "C" int kvs_decode_attn(const void* q, const void* k_cache, const void* v
     if (!q || !k_cache || !v_cache || !block_table || !n_tokens || !out || !lse || !workspace) return KVS_ERR_INVALID_ARG;
     if ((((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) & 15) != 0 || ((uintptr_t)workspace & 255) != 0)
         return KVS_ERR_ALIGNMENT;
-    if (workspace_bytes < kvs_decode_workspace_bytes(num_seqs, Hq, head_dim, num_splits)) return KVS_ERR_WORKSPACE;
+    const size_t plain = kvs_decode_workspace_bytes(num_seqs, Hq, head_dim, num_splits);
+    if (workspace_bytes < plain + (token_weight ? score_bytes(num_seqs, Hq, max_tokens) : 0)) return KVS_ERR_WORKSPACE;
     if (softmax_scale < 0.f || softmax_scale != softmax_scale) return KVS_ERR_INVALID_ARG;
     DecodeParams p;
     p.q = (const __nv_bfloat16*)q;
@@ -1065,7 +1132,29 @@ extern "C" int kvs_decode_attn(const void* q, const void* k_cache, const void* v
     p.scale_log2 = s * 1.4426950408889634f;
     p.part_o = (float*)((char*)workspace + DEC_WS_HEADER);
     p.part_ml = p.part_o + (size_t)num_seqs * Hq * num_splits * head_dim;
+    p.scores = token_weight ? (float*)((char*)workspace + plain) : nullptr;
+    p.score_stride = token_weight ? (int)align_up((size_t)max_tokens, 128) : 0;
     cudaStream_t st = (cudaStream_t)stream;
-    return head_dim == 64 ? launch_decode<64>(p, Hq / Hkv, k_cache, v_cache, (__nv_bfloat16*)out, lse, st)
-                          : launch_decode<128>(p, Hq / Hkv, k_cache, v_cache, (__nv_bfloat16*)out, lse, st);
+    return head_dim == 64 ? launch_decode<64>(p, Hq / Hkv, k_cache, v_cache, (__nv_bfloat16*)out, lse, token_weight, st)
+                          : launch_decode<128>(p, Hq / Hkv, k_cache, v_cache, (__nv_bfloat16*)out, lse, token_weight, st);
+}
+
+extern "C" int kvs_decode_attn(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
+                               const int32_t* n_tokens, int num_seqs, int Hq, int Hkv, int head_dim, int page_size, int max_pages,
+                               int num_pages, float softmax_scale, int num_splits, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                               kvs_stream_t stream) {
+    return decode_call(q, k_cache, v_cache, block_table, n_tokens, num_seqs, Hq, Hkv, head_dim, page_size, max_pages, num_pages, softmax_scale, num_splits, 0,
+                       out, lse, nullptr, workspace, workspace_bytes, stream);
+}
+
+extern "C" int kvs_decode_attn_weights(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
+                                       const int32_t* n_tokens, int num_seqs, int Hq, int Hkv, int head_dim, int page_size, int max_pages,
+                                       int num_pages, float softmax_scale, int num_splits, int max_tokens, void* out, float* lse, float* token_weight,
+                                       void* workspace, size_t workspace_bytes, kvs_stream_t stream) {
+    if (max_tokens <= 0) return KVS_ERR_INVALID_ARG;
+    if (max_tokens > 0x7fffff00 || (long long)max_pages * page_size > 0x7fffff00LL || Hq > 8192) return KVS_ERR_UNSUPPORTED;
+    if (num_seqs > 0 && !token_weight) return KVS_ERR_INVALID_ARG;
+    if (((uintptr_t)token_weight & 3) != 0) return KVS_ERR_ALIGNMENT;
+    return decode_call(q, k_cache, v_cache, block_table, n_tokens, num_seqs, Hq, Hkv, head_dim, page_size, max_pages, num_pages, softmax_scale, num_splits,
+                       max_tokens, out, lse, token_weight, workspace, workspace_bytes, stream);
 }

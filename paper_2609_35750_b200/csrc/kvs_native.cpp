@@ -21,7 +21,8 @@ namespace {
 #define KVS_FUNCTIONS(X) \
     X(kvs_mask_meta_bytes) X(kvs_mask_meta) X(kvs_mask_meta_keys) X(kvs_mask_meta_evicted) X(kvs_attn_fwd) X(kvs_attn_fwd_packed) \
     X(kvs_attn_fwd_dual) X(kvs_attn_bwd) X(kvs_attn_bwd_packed) X(kvs_attn_bwd_workspace_bytes) X(kvs_permute_rows) X(kvs_rope_qk) \
-    X(kvs_cache_append) X(kvs_cache_append_tokens) X(kvs_cache_truncate) X(kvs_cache_evict_lowest) X(kvs_verify_drafts) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
+    X(kvs_cache_append) X(kvs_cache_append_tokens) X(kvs_cache_truncate) X(kvs_cache_evict_lowest) X(kvs_verify_drafts) X(kvs_decode_attn_weights) \
+    X(kvs_decode_weights_workspace_bytes) X(kvs_decode_attn_window) X(kvs_decode_window_num_splits) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
 #define KVS_POINTER(name) decltype(&::name) name = nullptr;
 struct Library {
     KVS_FUNCTIONS(KVS_POINTER)
@@ -415,6 +416,75 @@ int small(int64_t n, const char* name) {
     return (int)n;
 }
 
+// The cache that an attention call reads: sizes and addresses
+struct Cache {
+    int64_t S, P, pages, page, Hkv, d;
+    const void *k, *v;
+    const int32_t *table, *n;
+    Cache(PyObject* const* a, const at::Tensor& q) {
+        const at::Tensor &kc = tensor(a[0], "k_cache"), &vc = tensor(a[1], "v_cache"), &bt = tensor(a[2], "block_table"), &nt = tensor(a[3], "n_tokens");
+        dims(kc, 4, "k_cache");
+        dims(bt, 2, "block_table");
+        S = bt.size(0), P = bt.size(1), pages = kc.size(0), page = kc.size(1), Hkv = kc.size(2), d = kc.size(3);
+        k = checked(kc, "k_cache", BF16, {-1, -1, -1, -1}, q);
+        v = checked(vc, "v_cache", BF16, {pages, page, Hkv, d}, q);
+        table = (const int32_t*)checked(bt, "block_table", I32, {-1, -1}, q);
+        n = (const int32_t*)checked(nt, "n_tokens", I32, {S}, q);
+        for (int64_t i : {S, P, pages, page, Hkv, d}) small(i, "the cache");
+        small(P * page, "block_table");
+    }
+};
+
+// (q, k_cache, v_cache, block_table, n_tokens, window, sinks, scale, num_splits, out, lse, workspace, max_tokens, stream)
+PyObject* decode_window(PyObject* const* a) {
+    const at::Tensor& q = tensor(a[0], "q");
+    dims(q, 4, "q");
+    const On on(q, "q", a[13]);
+    const Cache c(a + 1, q);
+    const int64_t new_ = q.size(1), Hq = q.size(2);
+    const void* pq = checked(q, "q", BF16, {c.S, new_, Hq, c.d}, q);
+    const int window = whole(a[5]), sinks = whole(a[6]);
+    const float scale = real(a[7]);
+    const int S = (int)c.S, n = small(new_, "q"), H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[12]), most = given_most ? given_most : (int)(c.P * c.page);
+    int splits = whole(a[8]);
+    if (splits <= 0) splits = lib.kvs_decode_window_num_splits(S, n, H, (int)c.Hkv, most, window, sinks);
+    const at::Tensor ws = given(a[11]) ? tensor(a[11], "workspace") : bytes(lib.kvs_decode_workspace_bytes(small(c.S * new_, "q"), H, d, splits), q);
+    const at::Tensor out = out_of(a[9], "out", q), lse = out_of(a[10], "lse", {c.S, new_, Hq}, q, F32);
+    void *po = checked(out, "out", BF16, {c.S, new_, Hq, c.d}, q), *pws = checked(ws, "workspace", U8, {-1}, q);
+    float* pl = (float*)checked(lse, "lse", F32, {c.S, new_, Hq}, q);
+    const size_t wn = (size_t)ws.numel();
+    call("kvs_decode_attn_window", [&] {
+        return lib.kvs_decode_attn_window(pq, c.k, c.v, c.table, c.n, S, n, H, (int)c.Hkv, d, (int)c.page, (int)c.P, (int)c.pages, scale, window, sinks, splits, po,
+                                          pl, pws, wn, on.stream);
+    });
+    return tuple({wrap(out, a[9]), wrap(lse, a[10])});
+}
+
+// (q, k_cache, v_cache, block_table, n_tokens, token_weight, scale, num_splits, out, lse, workspace, max_tokens, stream)
+PyObject* decode_weights(PyObject* const* a) {
+    const at::Tensor &q = tensor(a[0], "q"), &w = tensor(a[5], "token_weight");
+    dims(q, 3, "q");
+    const On on(q, "q", a[12]);
+    const Cache c(a + 1, q);
+    const int64_t Hq = q.size(1);
+    const void* pq = checked(q, "q", BF16, {c.S, Hq, c.d}, q);
+    float* pw = (float*)checked(w, "token_weight", F32, {c.S, c.P * c.page}, q);
+    const float scale = real(a[6]);
+    const int S = (int)c.S, H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[11]), most = given_most ? given_most : (int)(c.P * c.page);
+    int splits = whole(a[7]);
+    if (splits <= 0) splits = lib.kvs_decode_num_splits(S, (int)c.Hkv, most);
+    const at::Tensor ws = given(a[10]) ? tensor(a[10], "workspace") : bytes(lib.kvs_decode_weights_workspace_bytes(S, H, d, splits, most), q);
+    const at::Tensor out = out_of(a[8], "out", q), lse = out_of(a[9], "lse", {c.S, Hq}, q, F32);
+    void *po = checked(out, "out", BF16, {c.S, Hq, c.d}, q), *pws = checked(ws, "workspace", U8, {-1}, q);
+    float* pl = (float*)checked(lse, "lse", F32, {c.S, Hq}, q);
+    const size_t wn = (size_t)ws.numel();
+    call("kvs_decode_attn_weights", [&] {
+        return lib.kvs_decode_attn_weights(pq, c.k, c.v, c.table, c.n, S, H, (int)c.Hkv, d, (int)c.page, (int)c.P, (int)c.pages, scale, splits, most, po, pl, pw,
+                                           pws, wn, on.stream);
+    });
+    return tuple({wrap(out, a[8]), wrap(lse, a[9])});
+}
+
 // (k_new, v_new, active, block_table, n_tokens, free_list, k_cache, v_cache, stream)
 PyObject* cache_append_tokens(PyObject* const* a) {
     const at::Tensor &k = tensor(a[0], "k_new"), &v = tensor(a[1], "v_new"), &table = tensor(a[3], "block_table"), &n = tensor(a[4], "n_tokens"),
@@ -550,6 +620,8 @@ PyMethodDef methods[] = {
     KVS_ENTRY(rope_qk, 9),
     KVS_ENTRY(cache_append, 15),
     KVS_ENTRY(decode, 16),
+    KVS_ENTRY(decode_window, 14),
+    KVS_ENTRY(decode_weights, 13),
     KVS_ENTRY(cache_append_tokens, 9),
     KVS_ENTRY(cache_truncate, 8),
     KVS_ENTRY(cache_evict_lowest, 11),
