@@ -8,7 +8,7 @@ namespace kvs {
 struct CacheHeader {            // the first 16 bytes of the free-list buffer
     int32_t top;                // number of free pages on the stack
     int32_t status;             // KVS_OK or an error recorded by a kernel
-    int32_t joined;             // kvs_cache_append_tokens: whether the tokens of the call in flight have their pages
+    int32_t refused;            // kvs_cache_append_tokens: the call in flight could not have its pages
     int32_t pad;
 };
 

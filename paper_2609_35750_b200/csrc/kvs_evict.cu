@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
     if (no == KVS_OK && total > top) no = KVS_ERR_WORKSPACE;
     __syncthreads();
     if (tid == 0) {
-        hdr->joined = no == KVS_OK;
+        hdr->refused = no != KVS_OK;
         if (no == KVS_OK) hdr->top = top - total;
         else set_status(&hdr->status, no);
     }
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(256) join_kernel(JoinParams p) {
     constexpr int PER = sizeof(T) / sizeof(__nv_bfloat16);
     const int words = p.row / PER;
     pdl_wait();
-    if (!hdr->joined) return;
+    if (hdr->refused) return;
     const long long items = (long long)p.S * p.n_new * words;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
         const long long token = i / words;

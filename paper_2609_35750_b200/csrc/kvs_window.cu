@@ -139,7 +139,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         tmem_relinquish();
     } else {
         if (tid < COLS) {
-            s_ref[tid] = WIN_UNSET;
+            s_ref[tid] = tid < cols ? WIN_UNSET : 0.f;       // columns past the last score 0 and never move
             s_at[tid] = tid < cols ? at0 + tid / G : -1;
         }
         // column c, 16-byte chunk of its row: box, then chunk ^ (c % 8) of the 128-byte row; columns past the last are zero
@@ -343,22 +343,34 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
 #pragma unroll
                     for (int c = 0; c < 16; ++c) sc[c0 + c] = __uint_as_float(r[c]) * p.scale_log2;
                 }
+            // in blocks of 8 columns, without a branch inside, so that a block's loads and exponentials overlap
             if (masked) {
 #pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (c < cols && !sees(j, s_at[c])) sc[c] = -INFINITY;
+                for (int c0 = 0; c0 < COLS; c0 += 8)
+                    if (c0 < cols) {
+#pragma unroll
+                        for (int c = c0; c < c0 + 8; ++c) sc[c] = sees(j, s_at[c]) ? sc[c] : -INFINITY;
+                    }
             }
             bool above = false;
 #pragma unroll
-            for (int c = 0; c < COLS; ++c)
-                if (c < cols) above |= sc[c] - s_ref[c] > 8.0f;
+            for (int c0 = 0; c0 < COLS; c0 += 8)
+                if (c0 < cols) {
+                    const float4 a = *reinterpret_cast<const float4*>(s_ref + c0), b = *reinterpret_cast<const float4*>(s_ref + c0 + 4);
+                    const float ref[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) above |= sc[c0 + c] - ref[c] > 8.0f;
+                }
             if (group_any(1, 128, above)) {
                 // the columns' maxima over the tile; the references that are too low move there
 #pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (c < cols) {
-                        const int m = __reduce_max_sync(0xffffffffu, window_order(sc[c]));
-                        if (lane == 0) s_wmax[warp * COLS + c] = window_unorder(m);
+                for (int c0 = 0; c0 < COLS; c0 += 8)
+                    if (c0 < cols) {
+#pragma unroll
+                        for (int c = c0; c < c0 + 8; ++c) {
+                            const int m = __reduce_max_sync(0xffffffffu, window_order(sc[c]));
+                            if (lane == 0) s_wmax[warp * COLS + c] = window_unorder(m);
+                        }
                     }
                 named_bar_sync(1, 128);
                 if (tid < cols) {
@@ -369,8 +381,11 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 }
                 named_bar_sync(1, 128);
 #pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (c < cols) l_part[c] *= s_alpha[c];
+                for (int c0 = 0; c0 < COLS; c0 += 8)
+                    if (c0 < cols) {
+#pragma unroll
+                        for (int c = c0; c < c0 + 8; ++c) l_part[c] *= c < cols ? s_alpha[c] : 1.f;
+                    }
                 if (it > 0) {                     // O^T row d = tid
                     for (int c0 = 0; c0 < cols; c0 += 16) {
                         uint32_t o[16];
@@ -387,11 +402,16 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             uint8_t* prow = sgen + SM::OFF_P + (tid >> 6) * QBOX + ((tid & 7) << 1);
             const int chunk = (tid & 63) >> 3;
 #pragma unroll
-            for (int c = 0; c < COLS; ++c)
-                if (c < cols) {
-                    const float w = fast_exp2(sc[c] - s_ref[c]);
-                    l_part[c] += w;
-                    *reinterpret_cast<__nv_bfloat16*>(prow + c * 128 + ((chunk ^ (c & 7)) << 4)) = __float2bfloat16(w);
+            for (int c0 = 0; c0 < COLS; c0 += 8)
+                if (c0 < cols) {
+                    const float4 a = *reinterpret_cast<const float4*>(s_ref + c0), b = *reinterpret_cast<const float4*>(s_ref + c0 + 4);
+                    const float ref[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float w = fast_exp2(sc[c0 + c] - ref[c]);
+                        l_part[c0 + c] += w;
+                        *reinterpret_cast<__nv_bfloat16*>(prow + (c0 + c) * 128 + ((chunk ^ c) << 4)) = __float2bfloat16(w);
+                    }
                 }
             if (!PAGES) asm volatile("cp.async.wait_group 0;" ::: "memory");
             to_patch = false;
