@@ -54,7 +54,8 @@ struct WinSmem {
     static constexpr int OFF_MISC = OFF_BAR + 64;                      // tmem base, abort flag, status, bad rows of the tile before
     static constexpr int OFF_REF = OFF_MISC + 64;                      // [COLS] reference, base-2 units
     static constexpr int OFF_AT = OFF_REF + COLS * 4;                  // [COLS] position of the column's token
-    static constexpr int OFF_ALPHA = OFF_AT + COLS * 4;                // [COLS]
+    static constexpr int OFF_ROW = OFF_AT + COLS * 4;                  // [COLS] its row among all (sequence, token, query head)
+    static constexpr int OFF_ALPHA = OFF_ROW + COLS * 4;               // [COLS]
     static constexpr int OFF_WMAX = OFF_ALPHA + COLS * 4;              // [4 warps][COLS]
     static constexpr int TOTAL = OFF_WMAX + COLS * 16;
     static constexpr int DYN_BYTES = TOTAL + 1024;                     // slack for the 1024-byte alignment
@@ -121,6 +122,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     volatile uint32_t* s_bad = reinterpret_cast<volatile uint32_t*>(sgen + SM::OFF_MISC + 16);           // [4]
     float* s_ref = reinterpret_cast<float*>(sgen + SM::OFF_REF);
     int* s_at = reinterpret_cast<int*>(sgen + SM::OFF_AT);
+    int* s_row = reinterpret_cast<int*>(sgen + SM::OFF_ROW);
     float* s_alpha = reinterpret_cast<float*>(sgen + SM::OFF_ALPHA);
     float* s_wmax = reinterpret_cast<float*>(sgen + SM::OFF_WMAX);
 
@@ -139,18 +141,24 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         tmem_relinquish();
     } else {
         if (tid < COLS) {
+            const int t = tid / G;
             s_ref[tid] = tid < cols ? WIN_UNSET : 0.f;       // columns past the last score 0 and never move
-            s_at[tid] = tid < cols ? at0 + tid / G : -1;
+            s_at[tid] = tid < cols ? at0 + t : -1;
+            s_row[tid] = tid < cols ? (s * p.n_new + tok0 + t) * p.Hq + g * G + (tid - t * G) : -1;
         }
+        named_bar_sync(1, 128);
         // column c, 16-byte chunk of its row: box, then chunk ^ (c % 8) of the 128-byte row; columns past the last are zero
-        for (int i = tid; i < COLS * (D / 8); i += 128) {
-            const int c = i / (D / 8), c16 = i % (D / 8);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (c < cols) {
-                const int t = c / G, h = c - t * G;
-                v = *reinterpret_cast<const uint4*>(p.q + (((size_t)s * p.n_new + tok0 + t) * p.Hq + g * G + h) * D + c16 * 8);
-            }
-            *reinterpret_cast<uint4*>(sgen + SM::OFF_Q + (c16 >> 3) * QBOX + c * 128 + (((c16 & 7) ^ (c & 7)) << 4)) = v;
+        constexpr int NQ = COLS * (D / 8) / 128;             // chunks a thread, all on their way before the first is stored
+        uint4 v[NQ];
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            const int i = tid + k * 128, row = s_row[i / (D / 8)];
+            v[k] = row >= 0 ? *reinterpret_cast<const uint4*>(p.q + (size_t)row * D + (i % (D / 8)) * 8) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            const int i = tid + k * 128, c = i / (D / 8), c16 = i % (D / 8);
+            *reinterpret_cast<uint4*>(sgen + SM::OFF_Q + (c16 >> 3) * QBOX + c * 128 + (((c16 & 7) ^ (c & 7)) << 4)) = v[k];
         }
         fence_proxy_async();
     }
@@ -452,11 +460,26 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             tc_fence_after();
             if (to_patch) patch(tile_at(my_tiles - 1) * 128);
         }
-        // row of column c among all (sequence, token, query head)
-        auto part_row = [&](int c) {
-            const int t = c / G;
-            return (((size_t)s * p.n_new + tok0 + t) * p.Hq + g * G + (c - t * G)) * p.nsplit + z;
-        };
+        // sums of 8 columns over the warp's lanes: the lanes halve the columns that they hold three times, then add twice
+#pragma unroll
+        for (int c0 = 0; c0 < COLS; c0 += 8)
+            if (c0 < cols) {
+                float v[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[c] = l_part[c0 + c];
+#pragma unroll
+                for (int half = 4; half > 0; half >>= 1) {
+                    const bool upper = lane & (half * 4);
+#pragma unroll
+                    for (int c = 0; c < half; ++c) {
+                        const float mine = upper ? v[c + half] : v[c], other = upper ? v[c] : v[c + half];
+                        v[c] = mine + __shfl_xor_sync(0xffffffffu, other, half * 4);
+                    }
+                }
+                v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+                v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
+                if ((lane & 3) == 0) s_wmax[warp * COLS + c0 + (lane >> 2)] = v[0];
+            }
         for (int c0 = 0; c0 < cols; c0 += 16) {
             uint32_t o[16];
             if (my_tiles > 0) {
@@ -468,22 +491,16 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             }
             if (tid < D) {
 #pragma unroll
-                for (int c = 0; c < 16; ++c)
-                    if (c0 + c < cols) p.part_o[part_row(c0 + c) * D + tid] = __uint_as_float(o[c]);
+                for (int c = 0; c < 16; ++c) {
+                    const int row = s_row[c0 + c];
+                    if (row >= 0) p.part_o[((size_t)row * p.nsplit + z) * D + tid] = __uint_as_float(o[c]);
+                }
             }
         }
-#pragma unroll
-        for (int c = 0; c < COLS; ++c)
-            if (c < cols) {
-                float v = l_part[c];
-#pragma unroll
-                for (int ofs = 16; ofs > 0; ofs >>= 1) v += __shfl_xor_sync(0xffffffffu, v, ofs);
-                if (lane == 0) s_wmax[warp * COLS + c] = v;
-            }
         named_bar_sync(1, 128);
         if (tid < cols) {
             const float ref = s_ref[tid];
-            float* ml = p.part_ml + part_row(tid) * 2;
+            float* ml = p.part_ml + ((size_t)s_row[tid] * p.nsplit + z) * 2;
             ml[0] = ref == WIN_UNSET ? -INFINITY : ref;
             ml[1] = flagged_sum(s_wmax[tid] + s_wmax[COLS + tid] + s_wmax[2 * COLS + tid] + s_wmax[3 * COLS + tid], *(volatile int32_t*)status);
         }
