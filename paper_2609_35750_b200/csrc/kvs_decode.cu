@@ -113,55 +113,103 @@ __global__ void __launch_bounds__(256) decode_merge_kernel(MergeParams p) {
     if (row < p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31);
 }
 
-// kvs_decode_attn_weights: token_weight[s, j] += sum over query heads of exp2(score - lse), the heads in order, so that the sums do
-// not depend on which CTA comes first.  In the same launch as the merge: its CTAs come first, the others have a sequence and WT_TOKENS
-// tokens each and form the sequence's lse from the splits themselves.  The scores (4 bytes a token and query head) were written by
-// the kernels that formed them and are read once: forming them again would take the K rows (256 bytes a token and KV head).
-constexpr int WT_PER = 4, WT_TOKENS = 256 * WT_PER;
+// kvs_decode_attn_weights: token_weight[s, j] += sum over query heads of exp2(score - lse), in a fixed order of the heads, so that the
+// sums do not depend on which CTA comes first.  In the same launch as the merge: its CTAs come first, the others have a sequence and
+// `steps` times WT_TOKENS tokens each (one step where there are few: the host chooses).  A CTA forms the sequence's lse from the splits
+// itself; then a warp has every eighth head, a lane four tokens of each.  The scores (4 bytes a token and query head) were written by the kernels that formed them and are read once; forming
+// them again would take the K rows (256 bytes a token and KV head).  Bound by latency for few sequences (a thread per token that went
+// through the heads and the splits one after the other took 18 us on two sequences of 2000 tokens with 32 heads, here 5), else by the
+// scores' way to memory and back.
+constexpr int WT_TOKENS = 256;
 struct WeightParams {
     const float* scores;
     const int32_t* n_tokens;
     float* weight;                   // [S, weight_stride]
-    int Hq, score_stride, merge_ctas, chunks;
+    int Hq, score_stride, merge_ctas, chunks, steps;
     int weight_stride;               // max_pages * page_size: no sequence has more tokens
 };
 template <int D, int PART>
-__global__ void __launch_bounds__(256) decode_merge_weights_kernel(MergeParams p, WeightParams w) {
-    extern __shared__ float s_lse[];                     // [Hq] in base-2 units
+__global__ void __launch_bounds__(256, 4) decode_merge_weights_kernel(MergeParams p, WeightParams w) {
+    __shared__ float s_sum[8][WT_TOKENS];
+    extern __shared__ float s_lse[];                      // [Hq] in base-2 units
     pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x < w.merge_ctas) {
-        const int row = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-        if (row < p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31);
+        const int row = blockIdx.x * 8 + warp;
+        if (row < p.rows) decode_merge_row<D, PART>(p, row, lane);
         return;
     }
-    const int s = (blockIdx.x - w.merge_ctas) / w.chunks, j0 = (blockIdx.x - w.merge_ctas - s * w.chunks) * WT_TOKENS + threadIdx.x;
+    const int s = (blockIdx.x - w.merge_ctas) / w.chunks, j_first = (blockIdx.x - w.merge_ctas - s * w.chunks) * WT_TOKENS * w.steps;
     const int n = min(max(w.n_tokens[s], 0), w.weight_stride);
-    if (n > w.score_stride || j0 - (int)threadIdx.x >= n) return;            // the same in the whole CTA
-    for (int h = threadIdx.x; h < w.Hq; h += blockDim.x) {
-        const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)s * w.Hq + h) * p.nsplit;
-        float M = -INFINITY, L = 0.f;
-        for (int z = 0; z < p.nsplit; ++z) M = fmaxf(M, __ldcg(ml + z).x);
-        for (int z = 0; z < p.nsplit; ++z) {
-            const float2 x = __ldcg(ml + z);
-            L += fabsf(x.y) * fast_exp2(x.x - M);                            // the sign says that the split met an error: the merge tells
+    if (n > w.score_stride || j_first >= n) return;       // the same in the whole CTA
+    // lse of the sequence's heads, a warp for a head
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + (size_t)s * w.Hq * p.nsplit;
+    for (int h0 = warp; h0 < w.Hq; h0 += 32) {
+        float2 y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool there = h0 + 8 * k < w.Hq && lane < p.nsplit;
+            y[k] = there ? __ldcg(ml + (size_t)(h0 + 8 * k) * p.nsplit + lane) : make_float2(-INFINITY, 0.f);
         }
-        s_lse[h] = M + log2f(L);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float M = y[k].x, L = fabsf(y[k].y);          // the sign of a sum says that the split met an error: the merge tells
+            for (int z = lane + 32; z < p.nsplit && h0 + 8 * k < w.Hq; z += 32) {
+                const float2 x = __ldcg(ml + (size_t)(h0 + 8 * k) * p.nsplit + z);
+                const float m = fmaxf(M, x.x), mu = m == -INFINITY ? 0.f : m;
+                L = L * fast_exp2(M - mu) + fabsf(x.y) * fast_exp2(x.x - mu);
+                M = m;
+            }
+            float top = M;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            L *= fast_exp2(M - (top == -INFINITY ? 0.f : top));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+            if (lane == 0 && h0 + 8 * k < w.Hq) s_lse[h0 + 8 * k] = top + log2f(L);
+        }
     }
     __syncthreads();
-    float* weight = w.weight + (size_t)s * w.weight_stride;
-    const float* sc = w.scores + (size_t)s * w.Hq * w.score_stride;
-    float sum[WT_PER] = {}, old[WT_PER];
+    for (int i = 0; i < w.steps; ++i) {
+        const int j0 = j_first + i * WT_TOKENS, j = j0 + (int)threadIdx.x;
+        if (j0 >= n) break;
+        // whole tiles of scores are there, so that four tokens are read at a time; what lies behind the last token is dropped below
+        const float4* sc = reinterpret_cast<const float4*>(w.scores + (size_t)s * w.Hq * w.score_stride + j0) + lane;
+        const int second = j0 + 128 < n ? 32 : 0;
+        float* weight = w.weight + (size_t)s * w.weight_stride + j;
+        const float old = j < n ? *weight : 0.f;
+        float4 sum[2] = {};
+        for (int h0 = warp; h0 < w.Hq; h0 += 32) {
+            float4 x[4][2];                               // four heads on their way before the first is used
 #pragma unroll
-    for (int i = 0; i < WT_PER; ++i) old[i] = j0 + i * 256 < n ? weight[j0 + i * 256] : 0.f;
-#pragma unroll 4
-    for (int h = 0; h < w.Hq; ++h) {
+            for (int k = 0; k < 4; ++k) {
+                const float4* row = sc + (size_t)min(h0 + 8 * k, w.Hq - 1) * (w.score_stride / 4);
+                x[k][0] = __ldcg(row);
+                x[k][1] = __ldcg(row + second);
+            }
 #pragma unroll
-        for (int i = 0; i < WT_PER; ++i)
-            if (j0 + i * 256 < n) sum[i] += fast_exp2(__ldcg(sc + (size_t)h * w.score_stride + j0 + i * 256) - s_lse[h]);
+            for (int k = 0; k < 4; ++k) {
+                const float lse = h0 + 8 * k < w.Hq ? s_lse[h0 + 8 * k] : INFINITY;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    sum[i].x += fast_exp2(x[k][i].x - lse);
+                    sum[i].y += fast_exp2(x[k][i].y - lse);
+                    sum[i].z += fast_exp2(x[k][i].z - lse);
+                    sum[i].w += fast_exp2(x[k][i].w - lse);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) *reinterpret_cast<float4*>(&s_sum[warp][k * 128 + lane * 4]) = sum[k];
+        __syncthreads();
+        if (j < n) {
+            float all = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) all += s_sum[k][threadIdx.x];
+            *weight = old + all;
+        }
+        __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < WT_PER; ++i)
-        if (j0 + i * 256 < n) weight[j0 + i * 256] = old[i] + sum[i];
 }
 
 // A block-table entry is only followed if it names a page of the cache: anything else (a stale or
@@ -1081,10 +1129,13 @@ static int launch_decode(const DecodeParams& p, int G, const void* k_cache, cons
     const MergeParams m = {p.part_o, p.part_ml, out, lse, p.header, p.S * p.Hq, p.nsplit};
     const int merge_ctas = (m.rows + 7) / 8;
     if (!weight) return launch_decode_merge(m, D, st);
-    const int most = min(p.score_stride, p.max_pages * p.page_size), chunks = (most + WT_TOKENS - 1) / WT_TOKENS;
-    const WeightParams w = {p.scores, p.n_tokens, weight, p.Hq, p.score_stride, merge_ctas, chunks, p.max_pages * p.page_size};
+    const int most = min(p.score_stride, p.max_pages * p.page_size);
+    int steps = 1;
+    while (steps < 8 && (long long)p.S * ((most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps)) > 148 * 6) steps *= 2;
+    const int chunks = (most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps);
+    const WeightParams w = {p.scores, p.n_tokens, weight, p.Hq, p.score_stride, merge_ctas, chunks, steps, p.max_pages * p.page_size};
     if ((long long)merge_ctas + (long long)p.S * chunks > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
-    return launch_after(p.nsplit <= 4 ? decode_merge_weights_kernel<D, 4> : decode_merge_weights_kernel<D, 16>, merge_ctas + p.S * chunks, 256,
+    return launch_after(p.nsplit <= 4 ? decode_merge_weights_kernel<D, 4> : decode_merge_weights_kernel<D, 8>, merge_ctas + p.S * chunks, 256,
                         sizeof(float) * (size_t)p.Hq, st, m, w);
 }
 

@@ -19,8 +19,8 @@ namespace kvs {
 
 namespace cg = cooperative_groups;
 
-constexpr int VER_THREADS = 512;
-constexpr int VER_TILE = 256;               // tokens a warp adds up at a time: 8 loads of either row in flight a lane
+constexpr int VER_THREADS = 256;
+constexpr int VER_TILE = 512;               // tokens a warp adds up at a time: 16 loads of either row in flight a lane
 
 struct VerifyParams {
     const float* target;        // [S, n + 1, V]
@@ -36,14 +36,21 @@ struct VerifyParams {
 // weights of this lane's tokens of a tile, in 64 bits; no weight past the vocabulary, where the draft has more, or for a NaN
 __device__ __forceinline__ void verify_tile(const float* p, const float* q, int k0, int V, int lane, double (&w)[VER_TILE / 32]) {
     float a[VER_TILE / 32], b[VER_TILE / 32];
+    if (k0 + VER_TILE <= V && q) {               // a whole tile: all loads on their way before the first is used
 #pragma unroll
-    for (int i = 0; i < VER_TILE / 32; ++i) {
-        const int k = k0 + i * 32 + lane;
-        a[i] = k < V ? __ldg(p + k) : 0.f;
-        b[i] = (q && k < V) ? __ldg(q + k) : 0.f;
+        for (int i = 0; i < VER_TILE / 32; ++i) a[i] = __ldg(p + k0 + i * 32 + lane);
+#pragma unroll
+        for (int i = 0; i < VER_TILE / 32; ++i) b[i] = __ldg(q + k0 + i * 32 + lane);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VER_TILE / 32; ++i) {
+            const int k = k0 + i * 32 + lane;
+            a[i] = k < V ? __ldg(p + k) : 0.f;
+            b[i] = (q && k < V) ? __ldg(q + k) : 0.f;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < VER_TILE / 32; ++i) w[i] = fmax((double)a[i] - (double)b[i], 0.0);
+    for (int i = 0; i < VER_TILE / 32; ++i) w[i] = a[i] > b[i] ? (double)a[i] - (double)b[i] : 0.0;
 }
 
 __global__ void __launch_bounds__(VER_THREADS) verify_kernel(VerifyParams p) {
@@ -190,7 +197,7 @@ extern "C" int kvs_verify_drafts(const float* target_probs, const float* draft_p
         return KVS_ERR_ALIGNMENT;
     const int tiles = (vocab + VER_TILE - 1) / VER_TILE;
     int C = 8;
-    while (C > 1 && ((long long)num_seqs * C >= 4 * 148 || tiles < C)) C >>= 1;
+    while (C > 1 && ((long long)num_seqs * C >= 8 * 148 || tiles < C)) C >>= 1;
     if (vocab > (1 << 21)) C = 8;                // the tiles' sums fit into shared memory
     VerifyParams p = {target_probs, draft_probs, draft_tokens, u_accept, u_sample, tokens, n_accepted, n_draft, vocab, (tiles + C - 1) / C * VER_TILE};
     const size_t smem = (size_t)(p.part / VER_TILE) * sizeof(double);
