@@ -29,6 +29,8 @@ __device__ __forceinline__ int pages_of(int tokens, int page_size) { return (int
 // table and weights are written back in order: all reads are over before the first write.
 // Bound by latency: 4 bytes a token are read and written (64 caches of 32768 tokens: 2.6 us of HBM time).
 constexpr int EV_THREADS = 512;
+constexpr int EV_COPIES = 8;                // of the counts, by lane: scores crowd into a few digits
+constexpr int EV_MOST_CTAS = 8;             // of a cluster
 constexpr int EV_MOST_SMEM = 208 * 1024;
 
 struct EvictParams {
@@ -55,6 +57,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) evict_plan_kernel(EvictParams p)
     __shared__ int s_warp[33];
     CacheHeader* hdr = reinterpret_cast<CacheHeader*>(p.free_buf);
     pdl_wait();
+    const int top = hdr->top;
     int sum = 0, total;
     for (int s = threadIdx.x; s < p.S; s += PLAN_THREADS) {
         const int n = p.n_tokens[s];
@@ -62,7 +65,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) evict_plan_kernel(EvictParams p)
         else set_status(&hdr->status, KVS_ERR_INVALID_ARG);          // a length that the table cannot hold: this sequence stays as it is
     }
     block_prefix(sum, s_warp, total);
-    const int top = hdr->top;
     const bool fits = top >= 0 && total <= p.num_pages - top;        // else more pages would come back than the cache has: nothing is done
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -86,10 +88,12 @@ __device__ __forceinline__ uint32_t score_bits(float x) {
 
 __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int cap) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    __shared__ int s_hist[2][256];
+    __shared__ int s_hist[2][256];               // digits of this CTA's candidates, for the cluster
+    __shared__ __align__(16) int s_count[256 * EV_COPIES];
     __shared__ int s_warp[33];
+    __shared__ unsigned long long s_warp64[33];
     __shared__ int s_bin, s_below, s_in_bin;
-    __shared__ int s_counts[2];
+    __shared__ int2 s_counts;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
     const int s = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31;
@@ -115,9 +119,11 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     const int per = (live + C - 1) / C, first = min(c * per, live), count = min(first + per, live) - first;
     int32_t* table = p.block_table + (size_t)s * p.max_pages;
     float* weight = p.weight + (size_t)s * p.max_pages * ps;
+#pragma unroll 8
     for (int i = tid; i < count; i += EV_THREADS) s_page[i] = table[first + i];
+#pragma unroll 8
     for (int i = tid; i < count * ps; i += EV_THREADS) s_w[i] = weight[(size_t)first * ps + i];
-    if (tid < 256) s_hist[0][tid] = s_hist[1][tid] = 0;
+    for (int i = tid; i < 256 * EV_COPIES; i += EV_THREADS) s_count[i] = 0;
     __syncthreads();
     if (ps > 1) {
         for (int i = tid; i < count; i += EV_THREADS) {
@@ -135,27 +141,27 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     for (int pass = 0; pass < 4; ++pass) {
         const int shift = 24 - 8 * pass;
         int* hist = s_hist[pass & 1];
-        for (int i0 = 0; i0 < count; i0 += EV_THREADS) {
-            const int i = i0 + tid;
-            uint32_t key = 0;
-            bool in = i < count && candidate(i);
-            if (in) {
-                key = key_of(i);
-                in = pass == 0 || (key >> (shift + 8)) == (found >> (shift + 8));
-            }
-            // scores crowd into a few digits: equal ones of a warp are counted together
-            const unsigned alive = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const int digit = (int)((key >> shift) & 255u);
-                const unsigned same = __match_any_sync(alive, digit);
-                if (lane == __ffs(same) - 1) atomicAdd(&hist[digit], __popc(same));
-            }
+#pragma unroll 4
+        for (int i = tid; i < count; i += EV_THREADS) {
+            const uint32_t key = key_of(i);
+            if (candidate(i) && (pass == 0 || (key >> (shift + 8)) == (found >> (shift + 8))))
+                atomicAdd(&s_count[((key >> shift) & 255u) * EV_COPIES + (lane & (EV_COPIES - 1))], 1);
+        }
+        __syncthreads();
+        if (tid < 256) {
+            int4* copies = reinterpret_cast<int4*>(s_count + tid * EV_COPIES);
+            const int4 x = copies[0], y = copies[1];
+            hist[tid] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+            copies[0] = copies[1] = make_int4(0, 0, 0, 0);
         }
         cluster.sync();
         int sum = 0;
         if (tid < 256) {
-            for (int i = 0; i < C; ++i) sum += cluster.map_shared_rank(hist, i)[tid];
-            s_hist[(pass + 1) & 1][tid] = 0;             // all have read it: it was the one before this synchronisation
+            int part[EV_MOST_CTAS];                      // all on their way before the first is added: a remote read takes most of a microsecond
+#pragma unroll
+            for (int i = 0; i < EV_MOST_CTAS; ++i) part[i] = i < C ? cluster.map_shared_rank(hist, i)[tid] : 0;
+#pragma unroll
+            for (int i = 0; i < EV_MOST_CTAS; ++i) sum += part[i];
         }
         int all;
         const int below = block_prefix(sum, s_warp, all);
@@ -174,7 +180,8 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
         __syncthreads();
     }
     // ---- which pages leave, and where the others go ----
-    const int run = (count + EV_THREADS - 1) / EV_THREADS, a = min(tid * run, count), z = min(a + run, count);
+    const int run = (count + EV_THREADS - 1) / EV_THREADS | 1;           // odd: the threads' pages lie in different banks
+    const int a = min(tid * run, count), z = min(a + run, count);
     int under = 0, on = 0;
     for (int i = a; i < z; ++i)
         if (candidate(i)) {
@@ -182,22 +189,24 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
             under += key < found;
             on += key == found;
         }
-    int under_all, on_all;
-    int under_before = block_prefix(under, s_warp, under_all), on_before = block_prefix(on, s_warp, on_all);
-    if (tid == 0) {
-        s_counts[0] = under_all;
-        s_counts[1] = on_all;
-    }
+    unsigned long long both;                             // the two counts side by side
+    const unsigned long long before = block_prefix((unsigned long long)under << 32 | (unsigned)on, s_warp64, both);
+    const int under_all = (int)(both >> 32), on_all = (int)(both & 0xffffffffu);
+    int under_before = (int)(before >> 32), on_before = (int)(before & 0xffffffffu);
+    if (tid == 0) s_counts = make_int2(under_all, on_all);
     cluster.sync();
     int under_first = 0, on_first = 0, on_total = 0, under_total = 0;
-    for (int i = 0; i < C; ++i) {
-        const int* other = cluster.map_shared_rank(s_counts, i);
+    int2 other[EV_MOST_CTAS];
+#pragma unroll
+    for (int i = 0; i < EV_MOST_CTAS; ++i) other[i] = i < C ? *cluster.map_shared_rank(&s_counts, i) : make_int2(0, 0);
+#pragma unroll
+    for (int i = 0; i < EV_MOST_CTAS; ++i) {
         if (i < c) {
-            under_first += other[0];
-            on_first += other[1];
+            under_first += other[i].x;
+            on_first += other[i].y;
         }
-        under_total += other[0];
-        on_total += other[1];
+        under_total += other[i].x;
+        on_total += other[i].y;
     }
     const int of_equals = min(take - under_total, on_total);     // of those on the threshold the earlier slots leave
     under_before += under_first;
@@ -216,16 +225,17 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
                 ++on_before;
             }
         }
-        if (leaves) {
-            stack[-rank] = s_page[i];
-            if (evicted) evicted[rank] = first + i;
-        } else {
-            s_src[i - (rank - gone_first)] = (uint16_t)i;
-        }
+        // pages that stay from the front of the list, pages that leave from its end
+        s_src[leaves ? count - 1 - (rank - gone_first) : i - (rank - gone_first)] = (uint16_t)i;
     }
     __syncthreads();
     const int gone_here = under_all + min(on_first + on_all, of_equals) - min(on_first, of_equals);
     const int stays = count - gone_here, to = first - gone_first;        // page k that stays goes to slot `to + k`
+    for (int k = tid; k < gone_here; k += EV_THREADS) {
+        const int src = s_src[count - 1 - k];
+        stack[-(gone_first + k)] = s_page[src];
+        if (evicted) evicted[gone_first + k] = first + src;
+    }
     for (int k = tid; k < stays; k += EV_THREADS) {
         const int src = s_src[k];
         if (to + k != first + src) table[to + k] = s_page[src];
@@ -265,6 +275,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
     pdl_wait();
     auto joins = [&](int s) { return s < p.S && (!p.active || p.active[s]); };
     auto needs = [&](int n) { return pages_of(n + p.n_new, p.page_size) - pages_of(n, p.page_size); };
+    const int top = hdr->top;
     int sum = 0, total;
     for (int s = tid; s < p.S; s += PLAN_THREADS) {
         if (!joins(s)) continue;
@@ -275,7 +286,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
         else sum += needs(n);
     }
     block_prefix(sum, s_warp, total);                    // its synchronisations order s_no too
-    const int top = hdr->top;
     int no = s_no;
     if (no == KVS_OK && (top < 0 || top > p.num_pages)) no = KVS_ERR_INVALID_ARG;
     if (no == KVS_OK && total > top) no = KVS_ERR_WORKSPACE;
@@ -354,13 +364,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) truncate_kernel(int n_drafted, c
         }
         return n_drafted - kept;
     };
+    const int top = hdr->top;
     int sum = 0, total;
     for (int s = tid; s < S; s += PLAN_THREADS) {
         const int n = n_tokens[s], gone = leaves(s, n, true);
         sum += gone > 0 ? pages_of(n, page_size) - pages_of(n - gone, page_size) : 0;
     }
     block_prefix(sum, s_warp, total);
-    const int top = hdr->top;
     const bool fits = top >= 0 && total <= num_pages - top;
     __syncthreads();
     if (tid == 0) {
@@ -407,7 +417,10 @@ extern "C" int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recen
     // the cluster holds a sequence's weights, table and scores in shared memory
     const long long page_bytes = 4ll * page_size + 6 + (page_size > 1 ? 4 : 0);
     int C = 1;
-    while (C < 8 && ((long long)max_pages * page_size > 1024ll * C || ((long long)(max_pages + C - 1) / C + 2) * page_bytes > EV_MOST_SMEM)) C <<= 1;
+    // more CTAs where a sequence has more than 1024 tokens for each and two CTAs an SM are not yet taken, or where it does not fit
+    while (C < EV_MOST_CTAS && (((long long)max_pages * page_size > 1024ll * C && (long long)num_seqs * C < 148) ||
+                                ((long long)(max_pages + C - 1) / C + 2) * page_bytes > EV_MOST_SMEM))
+        C <<= 1;
     const int cap = (max_pages + C - 1) / C;
     const size_t smem = (size_t)((cap + 2) * page_bytes);
     if (smem > EV_MOST_SMEM || cap > 65535) return KVS_ERR_UNSUPPORTED;
