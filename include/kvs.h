@@ -407,9 +407,11 @@ int kvs_decode_attn(const void* q, const void* k_cache, const void* v_cache,
  *   out[s,t,h] = softmax_j(scale * q[s,t,h].k_j) v_j, lse[s,t,h] = log sum_j exp(scale * q.k_j)
  * q, out: bf16 [num_seqs, n_new, Hq, head_dim]; lse: fp32 [num_seqs, n_new, Hq].  Hq/Hkv <= 64.  A query that sees nothing (a sequence
  * with fewer live tokens than n_new) gets out = 0, lse = -inf.  Keys that a query does not see do not reach its result, whatever they hold.
- * num_splits: kvs_decode_window_num_splits gives one that fills the GPU.  workspace: >= kvs_decode_workspace_bytes(num_seqs * n_new, Hq,
- * head_dim, num_splits), 256-byte aligned.  Everything else as in kvs_decode_attn.
+ * num_splits: in how many parts at most, and one more, a head's keys are shared out among CTAs; kvs_decode_window_num_splits gives one that
+ * fills the GPU (more only need more workspace).  workspace: >= kvs_decode_window_workspace_bytes(...), 256-byte aligned.
+ * Everything else as in kvs_decode_attn.
  */
+size_t kvs_decode_window_workspace_bytes(int num_seqs, int n_new, int Hq, int Hkv, int head_dim, int num_splits);
 int kvs_decode_window_num_splits(int num_seqs, int n_new, int Hq, int Hkv, int max_tokens, int window, int sinks);
 int kvs_decode_attn_window(const void* q, const void* k_cache, const void* v_cache,
                            const int32_t* block_table, const int32_t* n_tokens,

@@ -68,6 +68,7 @@ SIGNATURES = {
     "kvs_decode_num_splits": (_i, [_i, _i, _i]),
     "kvs_decode_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "kvs_decode_attn": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _f, _i, _vp, _vp, _vp, _sz, _vp]),
+    "kvs_decode_window_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "kvs_decode_window_num_splits": (_i, [_i, _i, _i, _i, _i, _i, _i]),
     "kvs_decode_attn_window": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _f, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "kvs_decode_weights_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),

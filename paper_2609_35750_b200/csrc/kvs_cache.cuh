@@ -21,10 +21,8 @@ struct MergeParams {
     __nv_bfloat16* out;
     float* lse;
     int32_t* header;
-    int rows, nsplit;
+    int rows, nsplit;                    // nsplit: splits that there is room for
 };
-// the merge of a decode call, in kvs_decode.cu
-int launch_decode_merge(const MergeParams& m, int head_dim, cudaStream_t st);
 
 #ifdef __CUDACC__
 // launch_after with clusters of `cluster` CTAs along x
@@ -58,6 +56,63 @@ __device__ __forceinline__ float sum_and_status(float flagged, int32_t* status) 
     const uint32_t bits = __float_as_uint(flagged);
     if (bits >> 31) set_status(status, bits & 1u ? KVS_ERR_TIMEOUT : KVS_ERR_INVALID_ARG);
     return __uint_as_float(bits & 0x7fffffffu);
+}
+// Merge of the `count` splits (of p.nsplit that there is room for) of a (sequence, query head) by a warp: weights exp2(m_z - max), normalised, bf16 out and fp32 lse.  Bound by
+// latency: the loads of PART splits are on their way before the first is used (16: with 4 at a time 47 splits took 7 us more);
+// where there are few splits, PART = 4 leaves room for twice the warps (100 sequences of 64 heads, one split: step 38.0 ->
+// 34.8 us).  A kernel of its own, started by programmatic dependent launch: merging in the last CTA of a (sequence, KV head) to
+// finish, with counts in the workspace, cost every CTA a fence and an atomic and the merge its parallelism (a step in a CUDA
+// graph, merge in the last CTA -> here, us: 1 x 24000 tokens with 8 heads on 1 29.6 -> 15.0, 1 x 2000 with 32 on 8 14.2 -> 12.7,
+// 100 x 300 with 8 on 8 and head_dim 64 17.4 -> 13.5; launched call by call 30.4 -> 15.8, 14.6 -> 13.3, 17.9 -> 13.8).
+template <int D, int PART>
+__device__ __forceinline__ void decode_merge_row(const MergeParams& p, size_t row, int lane, int count) {
+    constexpr int PER = D / 32;
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + row * p.nsplit;
+    const float* po = p.part_o + row * p.nsplit * D + lane * PER;
+    float M = -INFINITY;
+    for (int z = lane; z < count; z += 32) M = fmaxf(M, __ldcg(ml + z).x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    const float Mu = (M == -INFINITY) ? 0.f : M;
+    float L = 0.f, acc[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] = 0.f;
+    for (int z0 = 0; z0 < count; z0 += 32) {
+        const float2 x = (z0 + lane < count) ? __ldcg(ml + z0 + lane) : make_float2(-INFINITY, 0.f);
+        const float w = fast_exp2(x.x - Mu);
+        L += sum_and_status(x.y, p.header + 1) * w;
+        for (int i0 = 0; i0 < min(32, count - z0); i0 += PART) {
+            float v[PART][PER];
+#pragma unroll
+            for (int i = 0; i < PART; ++i) {
+                const float* src = po + (size_t)(z0 + i0 + i) * D;
+                const bool there = z0 + i0 + i < count;
+                if constexpr (PER == 4) {
+                    const float4 y = there ? __ldcg(reinterpret_cast<const float4*>(src)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    v[i][0] = y.x; v[i][1] = y.y; v[i][2] = y.z; v[i][3] = y.w;
+                } else {
+                    const float2 y = there ? __ldcg(reinterpret_cast<const float2*>(src)) : make_float2(0.f, 0.f);
+                    v[i][0] = y.x; v[i][1] = y.y;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < PART; ++i) {
+                const float wi = __shfl_sync(0xffffffffu, w, i0 + i);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) acc[e] += v[i][e] * wi;
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] *= inv;
+    if constexpr (PER == 4)
+        *reinterpret_cast<uint2*>(p.out + row * D + lane * PER) = make_uint2(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]));
+    else
+        *reinterpret_cast<uint32_t*>(p.out + row * D + lane * PER) = pack_bf16(acc[0], acc[1]);
+    if (lane == 0) p.lse[row] = (L > 0.f) ? M * 0.6931471805599453f + logf(L) : -INFINITY;
 }
 // TMA gather: the 64-column slice starting at column c0 of the four rows r0..r3 of a 2-D tensor lands in four
 // consecutive 128-byte rows at dst (swizzled by address like a tiled box); completes 512 bytes on the barrier.

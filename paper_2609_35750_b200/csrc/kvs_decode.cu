@@ -48,69 +48,11 @@ __device__ __forceinline__ void decode_header(const DecodeParams& p) {
     }
 }
 
-// Merge of the splits of a (sequence, query head) by a warp: weights exp2(m_z - max), normalised, bf16 out and fp32 lse.  Bound by
-// latency: the loads of PART splits are on their way before the first is used (16: with 4 at a time 47 splits took 7 us more);
-// where there are few splits, PART = 4 leaves room for twice the warps (100 sequences of 64 heads, one split: step 38.0 ->
-// 34.8 us).  A kernel of its own, started by programmatic dependent launch: merging in the last CTA of a (sequence, KV head) to
-// finish, with counts in the workspace, cost every CTA a fence and an atomic and the merge its parallelism (a step in a CUDA
-// graph, merge in the last CTA -> here, us: 1 x 24000 tokens with 8 heads on 1 29.6 -> 15.0, 1 x 2000 with 32 on 8 14.2 -> 12.7,
-// 100 x 300 with 8 on 8 and head_dim 64 17.4 -> 13.5; launched call by call 30.4 -> 15.8, 14.6 -> 13.3, 17.9 -> 13.8).
-// (MergeParams: kvs_cache.cuh)
-template <int D, int PART>
-__device__ __forceinline__ void decode_merge_row(const MergeParams& p, size_t row, int lane) {
-    constexpr int PER = D / 32;
-    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + row * p.nsplit;
-    const float* po = p.part_o + row * p.nsplit * D + lane * PER;
-    float M = -INFINITY;
-    for (int z = lane; z < p.nsplit; z += 32) M = fmaxf(M, __ldcg(ml + z).x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    const float Mu = (M == -INFINITY) ? 0.f : M;
-    float L = 0.f, acc[PER];
-#pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-    for (int z0 = 0; z0 < p.nsplit; z0 += 32) {
-        const float2 x = (z0 + lane < p.nsplit) ? __ldcg(ml + z0 + lane) : make_float2(-INFINITY, 0.f);
-        const float w = fast_exp2(x.x - Mu);
-        L += sum_and_status(x.y, p.header + 1) * w;
-        for (int i0 = 0; i0 < min(32, p.nsplit - z0); i0 += PART) {
-            float v[PART][PER];
-#pragma unroll
-            for (int i = 0; i < PART; ++i) {
-                const float* src = po + (size_t)(z0 + i0 + i) * D;
-                const bool there = z0 + i0 + i < p.nsplit;
-                if constexpr (PER == 4) {
-                    const float4 y = there ? __ldcg(reinterpret_cast<const float4*>(src)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    v[i][0] = y.x; v[i][1] = y.y; v[i][2] = y.z; v[i][3] = y.w;
-                } else {
-                    const float2 y = there ? __ldcg(reinterpret_cast<const float2*>(src)) : make_float2(0.f, 0.f);
-                    v[i][0] = y.x; v[i][1] = y.y;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < PART; ++i) {
-                const float wi = __shfl_sync(0xffffffffu, w, i0 + i);
-#pragma unroll
-                for (int e = 0; e < PER; ++e) acc[e] += v[i][e] * wi;
-            }
-        }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-    const float inv = L > 0.f ? 1.f / L : 0.f;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] *= inv;
-    if constexpr (PER == 4)
-        *reinterpret_cast<uint2*>(p.out + row * D + lane * PER) = make_uint2(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]));
-    else
-        *reinterpret_cast<uint32_t*>(p.out + row * D + lane * PER) = pack_bf16(acc[0], acc[1]);
-    if (lane == 0) p.lse[row] = (L > 0.f) ? M * 0.6931471805599453f + logf(L) : -INFINITY;
-}
 template <int D, int PART>
 __global__ void __launch_bounds__(256) decode_merge_kernel(MergeParams p) {
     pdl_wait();
     const int row = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    if (row < p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31);
+    if (row < p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31, p.nsplit);
 }
 
 // kvs_decode_attn_weights: token_weight[s, j] += sum over query heads of exp2(score - lse), in a fixed order of the heads, so that the
@@ -136,7 +78,7 @@ __global__ void __launch_bounds__(256, 4) decode_merge_weights_kernel(MergeParam
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x < w.merge_ctas) {
         const int row = blockIdx.x * 8 + warp;
-        if (row < p.rows) decode_merge_row<D, PART>(p, row, lane);
+        if (row < p.rows) decode_merge_row<D, PART>(p, row, lane, p.nsplit);
         return;
     }
     const int s = (blockIdx.x - w.merge_ctas) / w.chunks, j_first = (blockIdx.x - w.merge_ctas - s * w.chunks) * WT_TOKENS * w.steps;
@@ -1114,21 +1056,13 @@ static int launch_partials(const DecodeParams& p, int G, const void* k_cache, co
     return KVS_OK;
 }
 
-namespace kvs {
-int launch_decode_merge(const MergeParams& m, int head_dim, cudaStream_t st) {
-    const int ctas = (m.rows + 7) / 8;
-    if (head_dim == 64) return launch_after(m.nsplit <= 4 ? decode_merge_kernel<64, 4> : decode_merge_kernel<64, 16>, ctas, 256, 0, st, m);
-    return launch_after(m.nsplit <= 4 ? decode_merge_kernel<128, 4> : decode_merge_kernel<128, 16>, ctas, 256, 0, st, m);
-}
-}  // namespace kvs
-
 template <int D>
 static int launch_decode(const DecodeParams& p, int G, const void* k_cache, const void* v_cache, __nv_bfloat16* out, float* lse, float* weight, cudaStream_t st) {
     const int rc = weight ? launch_partials<D, true>(p, G, k_cache, v_cache, st) : launch_partials<D, false>(p, G, k_cache, v_cache, st);
     if (rc != KVS_OK) return rc;
     const MergeParams m = {p.part_o, p.part_ml, out, lse, p.header, p.S * p.Hq, p.nsplit};
     const int merge_ctas = (m.rows + 7) / 8;
-    if (!weight) return launch_decode_merge(m, D, st);
+    if (!weight) return launch_after(p.nsplit <= 4 ? decode_merge_kernel<D, 4> : decode_merge_kernel<D, 16>, merge_ctas, 256, 0, st, m);
     const int most = min(p.score_stride, p.max_pages * p.page_size);
     int steps = 1;
     while (steps < 8 && (long long)p.S * ((most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps)) > 148 * 6) steps *= 2;

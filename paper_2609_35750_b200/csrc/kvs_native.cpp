@@ -22,7 +22,7 @@ namespace {
     X(kvs_mask_meta_bytes) X(kvs_mask_meta) X(kvs_mask_meta_keys) X(kvs_mask_meta_evicted) X(kvs_attn_fwd) X(kvs_attn_fwd_packed) \
     X(kvs_attn_fwd_dual) X(kvs_attn_bwd) X(kvs_attn_bwd_packed) X(kvs_attn_bwd_workspace_bytes) X(kvs_permute_rows) X(kvs_rope_qk) \
     X(kvs_cache_append) X(kvs_cache_append_tokens) X(kvs_cache_truncate) X(kvs_cache_evict_lowest) X(kvs_verify_drafts) X(kvs_decode_attn_weights) \
-    X(kvs_decode_weights_workspace_bytes) X(kvs_decode_attn_window) X(kvs_decode_window_num_splits) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
+    X(kvs_decode_weights_workspace_bytes) X(kvs_decode_attn_window) X(kvs_decode_window_num_splits) X(kvs_decode_window_workspace_bytes) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
 #define KVS_POINTER(name) decltype(&::name) name = nullptr;
 struct Library {
     KVS_FUNCTIONS(KVS_POINTER)
@@ -448,7 +448,7 @@ PyObject* decode_window(PyObject* const* a) {
     const int S = (int)c.S, n = small(new_, "q"), H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[12]), most = given_most ? given_most : (int)(c.P * c.page);
     int splits = whole(a[8]);
     if (splits <= 0) splits = lib.kvs_decode_window_num_splits(S, n, H, (int)c.Hkv, most, window, sinks);
-    const at::Tensor ws = given(a[11]) ? tensor(a[11], "workspace") : bytes(lib.kvs_decode_workspace_bytes(small(c.S * new_, "q"), H, d, splits), q);
+    const at::Tensor ws = given(a[11]) ? tensor(a[11], "workspace") : bytes(lib.kvs_decode_window_workspace_bytes(S, n, H, (int)c.Hkv, d, splits), q);
     const at::Tensor out = out_of(a[9], "out", q), lse = out_of(a[10], "lse", {c.S, new_, Hq}, q, F32);
     void *po = checked(out, "out", BF16, {c.S, new_, Hq, c.d}, q), *pws = checked(ws, "workspace", U8, {-1}, q);
     float* pl = (float*)checked(lse, "lse", F32, {c.S, new_, Hq}, q);

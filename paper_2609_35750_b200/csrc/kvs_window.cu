@@ -5,9 +5,14 @@
 // products run on the tensor core in the transposed form, so that a tile's 128 keys fill its 128 rows and the few queries its columns:
 //   S^T [128 keys x N] = K [128 x d] Q^T            A = K tile, B = Q: column c is query head c % G of token c / G
 //   O^T [d x N]       += V^T [d x 128 keys] P^T     A = V tile read MN-major, B = P^T  (d = 64: rows 64 .. 127 repeat rows 0 .. 63)
-// One CTA per (split, KV head, sequence and group of new tokens): four softmax warps (a thread has a key of S^T and a column d of
-// O^T) and a control warp (block table, TMA loads, MMA issue).  K of tile t + 1 is asked for as soon as S^T of tile t is complete, V of
-// tile t as soon as the second product of tile t - 1 is; two or three CTAs an SM overlap one another's loads, products and softmax.
+// Four softmax warps (a thread has a key of S^T and a column d of O^T) and a control warp (block table, TMA loads, MMA issue).  K of
+// tile t + 1 is asked for as soon as S^T of tile t is complete, V of tile t as soon as the second product of tile t - 1 is; two or three
+// CTAs an SM overlap one another's loads, products and softmax.
+//
+// Every CTA has an equal share of all tiles: the tiles of (sequence and group of new tokens, KV head) follow one another, CTA c has
+// tiles c share .. (c + 1) share - 1 of them, whose heads end where they end.  Lengths are ragged and known on the device alone, so every
+// CTA adds them up itself; the first one leaves the sums for the merge, which finds from them which CTAs had a row.  K and V of the next
+// head are on their way while the last one's result is written.  Against CTAs of a fixed number per sequence (us): SHARE_FIGURES
 // Rows reach shared memory as in kvs_decode_attn: pages of 8 to 128 tokens that tile 128 by one TMA box each, others by rows (K by
 // TMA gather4, V by cp.async).
 //
@@ -29,6 +34,12 @@ constexpr int WIN_PAGES = 1;         // one TMA box per page
 constexpr int WIN_ROWS = 2;          // K: TMA gather4; V: cp.async rows
 constexpr float WIN_UNSET = -1e30f;  // reference of a column that has seen no key yet: any score is far above it
 
+struct WindowEntry {                 // of the workspace, written by the first CTA
+    long long before;                // tiles of the entries before it, for one KV head
+    int tiles, pad;
+};
+constexpr int WIN_SHARE_WORD = 2;    // the share, behind {magic, status} of the workspace's header
+
 struct WindowParams {
     const __nv_bfloat16* q;          // [S, n_new, Hq, D]
     const __nv_bfloat16* v_cache;    // [num_pages, page_size, Hkv, D]
@@ -36,6 +47,7 @@ struct WindowParams {
     const int32_t* n_tokens;         // [S]
     int S, n_new, Hq, Hkv, G, page_size, page_shift, max_pages, num_pages, nsplit;
     int groups, group_tokens;        // new tokens of a sequence in groups of group_tokens: G * group_tokens columns at most
+    WindowEntry* entries;            // [S * groups], for the merge
     int window, sinks;
     int32_t* header;
     float scale_log2;
@@ -43,8 +55,50 @@ struct WindowParams {
     float* part_ml;                  // [S * n_new * Hq, nsplit, 2]
 };
 
+// The tiles of a group of new tokens (entry e = sequence * groups + group), for one KV head.  Queries stand at at0 .. end - 1 (negative
+// ones see nothing); keys below `head` or in [lo, end) are seen by some of them.
+struct WindowUnit {
+    int s, tok0, cols, at0, end, head, lo, head_tiles, body, tiles;
+    __device__ __forceinline__ void load(const WindowParams& p, int e) {
+        s = e / p.groups;
+        const int group = e - s * p.groups, n = min(max(p.n_tokens[s], 0), p.max_pages * p.page_size);       // never past the sequence's table
+        tok0 = group * p.group_tokens;
+        const int ntok = min(p.group_tokens, p.n_new - tok0);
+        cols = ntok * p.G;
+        at0 = n - p.n_new + tok0;
+        end = max(at0 + ntok, 0);
+        head = min(p.sinks, end);
+        lo = max(0, max(at0, 0) - (p.window - 1));
+        head_tiles = (head + 127) >> 7;
+        body = max(lo >> 7, head_tiles);
+        tiles = head_tiles + max(0, ((end + 127) >> 7) - body);
+    }
+    __device__ __forceinline__ int key_of(int i) const { return (i < head_tiles ? i : body + (i - head_tiles)) * 128; }      // first key of tile i
+    __device__ __forceinline__ bool seen_by_some(int j) const { return j < head || (j >= lo && j < end); }
+};
+// A CTA's way through its share
+struct WindowCursor {
+    int e, g, i;                     // entry, KV head, tile
+    long long before;                // tiles of the entries before, for one KV head
+    WindowUnit u;
+    // to the first tile of the next head (or entry with any tile)
+    __device__ __forceinline__ void next_unit(const WindowParams& p) {
+        i = 0;
+        if (++g < p.Hkv) return;
+        g = 0;
+        do {
+            before += u.tiles;
+            u.load(p, ++e);
+        } while (u.tiles == 0);
+    }
+    __device__ __forceinline__ void next(const WindowParams& p) {
+        if (++i == u.tiles) next_unit(p);
+    }
+};
+
 template <int D, int COLS>
 struct WinSmem {
+    static constexpr int CTAS = COLS <= 16 || (COLS <= 32 && D == 64) ? 3 : 2;      // an SM
     static constexpr int TILE_BYTES = 128 * D * 2;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_V = TILE_BYTES;
@@ -53,9 +107,9 @@ struct WinSmem {
     static constexpr int OFF_BAR = OFF_P + COLS * 256;
     static constexpr int OFF_MISC = OFF_BAR + 64;                      // tmem base, abort flag, status, bad rows of the tile before
     static constexpr int OFF_REF = OFF_MISC + 64;                      // [COLS] reference, base-2 units
-    static constexpr int OFF_AT = OFF_REF + COLS * 4;                  // [COLS] position of the column's token
-    static constexpr int OFF_ROW = OFF_AT + COLS * 4;                  // [COLS] its row among all (sequence, token, query head)
-    static constexpr int OFF_ALPHA = OFF_ROW + COLS * 4;               // [COLS]
+    static constexpr int OFF_AT = OFF_REF + COLS * 4;                  // [2][COLS] position of the column's token, of two heads in turn
+    static constexpr int OFF_ROW = OFF_AT + COLS * 8;                  // [2][COLS] its row among all (sequence, token, query head)
+    static constexpr int OFF_ALPHA = OFF_ROW + COLS * 8;               // [COLS]
     static constexpr int OFF_WMAX = OFF_ALPHA + COLS * 4;              // [4 warps][COLS]
     static constexpr int TOTAL = OFF_WMAX + COLS * 16;
     static constexpr int DYN_BYTES = TOTAL + 1024;                     // slack for the 1024-byte alignment
@@ -81,7 +135,7 @@ __device__ __forceinline__ bool group_any(int id, int nthreads, bool mine) {
 }
 
 template <int D, int COLS, int LOAD>
-__global__ void __launch_bounds__(WIN_THREADS, COLS <= 16 || (COLS <= 32 && D == 64) ? 3 : 2)
+__global__ void __launch_bounds__(WIN_THREADS, WinSmem<D, COLS>::CTAS)
 decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ WindowParams p) {
     using SM = WinSmem<D, COLS>;
     constexpr int BOX = 16384, NBOX = D / 64;
@@ -89,33 +143,70 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     constexpr uint32_t IDESC_S = make_idesc(COLS, 0, 0), IDESC_O = make_idesc(COLS, 1, 0);
     constexpr bool PAGES = LOAD == WIN_PAGES;
     extern __shared__ uint8_t smem_raw[];
-    const int z = blockIdx.x, g = blockIdx.y, s = blockIdx.z / p.groups, group = blockIdx.z - s * p.groups;
+    __shared__ long long s_scan[33], s_before;
+    __shared__ int s_most, s_entry;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int ps = p.page_size, G = p.G, E = p.S * p.groups;
+    if (tid == 0) s_most = 0;
+    __syncthreads();
     pdl_wait();
-    if ((blockIdx.x | blockIdx.y | blockIdx.z | threadIdx.x) == 0) {
-        p.header[0] = (int32_t)WS_MAGIC;
-        p.header[1] = KVS_OK;
+    // ---- this CTA's share ----
+    long long share, at, all;
+    {
+        long long sum = 0;
+        int most = 0;
+        WindowUnit u;
+        for (int e = tid; e < E; e += WIN_THREADS) {
+            u.load(p, e);
+            sum += u.tiles;
+            most = max(most, u.tiles);
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0 && most > 0) atomicMax(&s_most, most);
+        block_prefix(sum, s_scan, all);
+        all *= p.Hkv;
+        // not so small that a head is cut into more parts than there is room for: the first may be cut anywhere
+        share = max(max((all + gridDim.x - 1) / gridDim.x, ((long long)s_most + p.nsplit - 3) / (p.nsplit - 1)), 1ll);
+        at = share * blockIdx.x;
+        if (blockIdx.x == 0 && tid == 0) {
+            p.header[0] = (int32_t)WS_MAGIC;
+            p.header[1] = KVS_OK;
+            *reinterpret_cast<long long*>(p.header + WIN_SHARE_WORD) = share;
+        }
+        if (at >= all && blockIdx.x != 0) return;          // the same in the whole CTA
+        long long run = 0, here;
+        for (int e0 = 0; e0 < E && (blockIdx.x == 0 || run * p.Hkv <= at); e0 += WIN_THREADS) {
+            const int e = e0 + tid;
+            u.tiles = 0;
+            if (e < E) u.load(p, e);
+            const long long before = run + block_prefix((long long)u.tiles, s_scan, here);
+            if (e < E && blockIdx.x == 0) p.entries[e] = {before, u.tiles, 0};
+            if (u.tiles > 0 && before * p.Hkv <= at && at < (before + u.tiles) * p.Hkv) {
+                s_entry = e;
+                s_before = before;
+            }
+            run += here;
+        }
+        __syncthreads();
+        if (at >= all) return;                             // the first CTA of a call without a tile
     }
-    const int ps = p.page_size, G = p.G;
-    const int n = min(max(p.n_tokens[s], 0), p.max_pages * ps);          // never past the sequence's table
-    const int tok0 = group * p.group_tokens, ntok = min(p.group_tokens, p.n_new - tok0), cols = ntok * G;
-    // positions of the group's queries: at0 .. end - 1 (negative ones see nothing); keys below `head` or in [lo, end) are seen by some
-    const int at0 = n - p.n_new + tok0, end = max(at0 + ntok, 0);
-    const int head = min(p.sinks, end);
-    const int lo = max(0, max(at0, 0) - (p.window - 1));
-    const int head_tiles = (head + 127) >> 7, body = max(lo >> 7, head_tiles);
-    const int all_tiles = head_tiles + max(0, ((end + 127) >> 7) - body);
-    const int per = (all_tiles + p.nsplit - 1) / p.nsplit;               // contiguous tiles per split
-    const int i_begin = min(z * per, all_tiles), my_tiles = min(i_begin + per, all_tiles) - i_begin;
-    auto tile_at = [&](int i) { return i_begin + i < head_tiles ? i_begin + i : body + (i_begin + i - head_tiles); };
-    auto seen_by_some = [&](int j) { return j < head || (j >= lo && j < end); };
+    const int my_tiles = (int)min(share, all - at);
+    WindowCursor start;
+    start.e = s_entry;
+    start.before = s_before;
+    start.u.load(p, start.e);
+    {
+        const long long into = at - start.before * p.Hkv;
+        start.g = (int)(into / start.u.tiles);
+        start.i = (int)(into - (long long)start.g * start.u.tiles);
+    }
 
     const uint32_t sraw = smem_u32(smem_raw), sbase = (sraw + 1023u) & ~1023u;
     uint8_t* sgen = smem_raw + (sbase - sraw);
     const uint32_t sK = sbase + SM::OFF_K, sV = sbase + SM::OFF_V, sQ = sbase + SM::OFF_Q, sP = sbase + SM::OFF_P, bars = sbase + SM::OFF_BAR;
     // as in the decode kernel: K / V rows have landed, S^T complete (hence K, and the V and P^T of the tile before, consumed), P^T
-    // written, second product complete
-    const uint32_t bar_kfull = bars, bar_vfull = bars + 8, bar_s = bars + 16, bar_p = bars + 24, bar_done = bars + 32;
+    // written, second product complete; and the queries of a head are in place
+    const uint32_t bar_kfull = bars, bar_vfull = bars + 8, bar_s = bars + 16, bar_p = bars + 24, bar_done = bars + 32, bar_q = bars + 40;
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(sgen + SM::OFF_MISC);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + SM::OFF_MISC + 4);
     int32_t* status = reinterpret_cast<int32_t*>(sgen + SM::OFF_MISC + 8);
@@ -134,39 +225,19 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         mbar_init(bar_s, 1);
         mbar_init(bar_p, 128);
         mbar_init(bar_done, 1);
+        mbar_init(bar_q, 128);
         fence_mbar_init();
     }
     if (warp == 4) {
         tmem_alloc(smem_u32(s_tmem), 2 * COLS);
         tmem_relinquish();
-    } else {
-        if (tid < COLS) {
-            const int t = tid / G;
-            s_ref[tid] = tid < cols ? WIN_UNSET : 0.f;       // columns past the last score 0 and never move
-            s_at[tid] = tid < cols ? at0 + t : -1;
-            s_row[tid] = tid < cols ? (s * p.n_new + tok0 + t) * p.Hq + g * G + (tid - t * G) : -1;
-        }
-        named_bar_sync(1, 128);
-        // column c, 16-byte chunk of its row: box, then chunk ^ (c % 8) of the 128-byte row; columns past the last are zero
-        constexpr int NQ = COLS * (D / 8) / 128;             // chunks a thread, all on their way before the first is stored
-        uint4 v[NQ];
-#pragma unroll
-        for (int k = 0; k < NQ; ++k) {
-            const int i = tid + k * 128, row = s_row[i / (D / 8)];
-            v[k] = row >= 0 ? *reinterpret_cast<const uint4*>(p.q + (size_t)row * D + (i % (D / 8)) * 8) : make_uint4(0, 0, 0, 0);
-        }
-#pragma unroll
-        for (int k = 0; k < NQ; ++k) {
-            const int i = tid + k * 128, c = i / (D / 8), c16 = i % (D / 8);
-            *reinterpret_cast<uint4*>(sgen + SM::OFF_Q + (c16 >> 3) * QBOX + c * 128 + (((c16 & 7) ^ (c & 7)) << 4)) = v[k];
-        }
-        fence_proxy_async();
+    } else if (tid < COLS) {
+        s_ref[tid] = tid < start.u.cols ? WIN_UNSET : 0.f;       // columns past the last score 0 and never move
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_S = *s_tmem, tmem_O = tmem_S + COLS;
-    const int32_t* bt = p.block_table + (size_t)s * p.max_pages;
     auto split_token = [&](int tok, int& entry, int& offset) {
         entry = p.page_shift >= 0 ? tok >> p.page_shift : tok / ps;
         offset = tok - entry * ps;
@@ -186,60 +257,69 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         const int ppt = PAGES ? 128 / ps : 0;                  // pages per tile
         // PAGES: lane i has page i of the tile, if some query sees a row of it; ROWS: lane L the pages of rows 4 L .. 4 L + 3 (rows past the
         // end repeat the last one: their scores are masked), if some query sees one of them
-        struct Ids { int v[PAGES ? 1 : 4]; bool need; };
-        auto fetch_ids = [&](int i, Ids& id) {
-            id.need = false;
-            if (i >= my_tiles) return;
-            const int k0 = tile_at(i) * 128;
-            const int a = k0 + lane * (PAGES ? ps : 4), e = min(a + (PAGES ? ps : 4), end);
-            id.need = (!PAGES || lane < ppt) && a < e && (a < head || e > lo);
-            if (PAGES) {
-                id.v[0] = id.need ? bt[tile_at(i) * ppt + lane] : 0;
-            } else if (id.need) {
+        struct Tile { int k0, end, g, v[PAGES ? 1 : 4]; bool need, first; };
+        WindowCursor c = start;
+        int left = my_tiles;
+        auto fetch = [&](Tile& t) {                            // the tile at the cursor, which moves on
+            t.need = false;
+            if (left == 0) return;
+            const int32_t* bt = p.block_table + (size_t)c.u.s * p.max_pages;
+            t.k0 = c.u.key_of(c.i);
+            t.end = c.u.end;
+            t.g = c.g;
+            t.first = left == my_tiles || c.i == 0;
+            const int a = t.k0 + lane * (PAGES ? ps : 4), e = min(a + (PAGES ? ps : 4), c.u.end);
+            t.need = (!PAGES || lane < ppt) && a < e && (a < c.u.head || e > c.u.lo);
+            if constexpr (PAGES) {
+                t.v[0] = t.need ? bt[(t.k0 >> 7) * ppt + lane] : 0;
+            } else if (t.need) {
 #pragma unroll
-                for (int j = 0; j < (PAGES ? 1 : 4); ++j) {
+                for (int j = 0; j < 4; ++j) {
                     int en, o;
-                    split_token(min(a + j, end - 1), en, o);
-                    id.v[j] = bt[en];
+                    split_token(min(a + j, c.u.end - 1), en, o);
+                    t.v[j] = bt[en];
                 }
             }
+            if (--left > 0) c.next(p);
         };
-        auto load_pages = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, const Ids& id) {
-            const uint32_t pages = __popc(__ballot_sync(0xffffffffu, id.need));
+        auto load_pages = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, const Tile& t) {
+            const uint32_t pages = __popc(__ballot_sync(0xffffffffu, t.need));
             if (leader) mbar_expect_tx(bar, pages * (uint32_t)(ps * D * 2));
             __syncwarp();
-            if (id.need) {
-                const int row = checked_page(id.v[0]) * ps;
+            if (t.need) {
+                const int row = checked_page(t.v[0]) * ps;
 #pragma unroll
-                for (int b = 0; b < NBOX; ++b) tma_load_3d(dst + b * BOX + (uint32_t)(lane * ps) * 128u, map, b * 64, g, row, bar);
+                for (int b = 0; b < NBOX; ++b) tma_load_3d(dst + b * BOX + (uint32_t)(lane * ps) * 128u, map, b * 64, t.g, row, bar);
             }
         };
-        auto load_k = [&](int i, const Ids& id) {              // K buffer must be free
+        auto load_k = [&](const Tile& t) {                     // K buffer must be free
             if constexpr (PAGES) {
-                load_pages(&tm_k, sK, bar_kfull, id);
+                load_pages(&tm_k, sK, bar_kfull, t);
             } else {
-                const uint32_t quads = __popc(__ballot_sync(0xffffffffu, id.need));
+                const uint32_t quads = __popc(__ballot_sync(0xffffffffu, t.need));
                 if (leader) mbar_expect_tx(bar_kfull, quads * (uint32_t)(4 * D * 2));
                 __syncwarp();
-                if (id.need) {
+                if (t.need) {
                     int row[4];
-    #pragma unroll
+#pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         int en, o;
-                        split_token(min(tile_at(i) * 128 + 4 * lane + j, end - 1), en, o);
-                        row[j] = checked_page(id.v[j]) * ps + o;
+                        split_token(min(t.k0 + 4 * lane + j, t.end - 1), en, o);
+                        row[j] = checked_page(t.v[j]) * ps + o;
                     }
-    #pragma unroll
-                    for (int b = 0; b < NBOX; ++b) tma_gather4(sK + b * BOX + (uint32_t)lane * 512u, &tm_k, g * D + b * 64, row[0], row[1], row[2], row[3], bar_kfull);
+#pragma unroll
+                    for (int b = 0; b < NBOX; ++b)
+                        tma_gather4(sK + b * BOX + (uint32_t)lane * 512u, &tm_k, t.g * D + b * 64, row[0], row[1], row[2], row[3], bar_kfull);
                 }
             }
         };
-        Ids cur, nxt;
-        for (int j = 0; j < (PAGES ? 1 : 4); ++j) cur.v[j] = nxt.v[j] = 0;
-        fetch_ids(0, cur);
-        fetch_ids(1, nxt);
-        if (my_tiles > 0) load_k(0, cur);
+        Tile cur = {}, nxt = {};
+        fetch(cur);
+        fetch(nxt);
+        load_k(cur);
+        int heads = 0;
         for (int it = 0; it < my_tiles; ++it) {
+            if (cur.first) mbar_wait(bar_q, heads++ & 1, abort_flag, status);
             mbar_wait(bar_kfull, it & 1, abort_flag, status);
             tc_fence_after();
 #pragma unroll
@@ -251,93 +331,132 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             if (leader) mma_commit(bar_s);
             mbar_wait(bar_s, it & 1, abort_flag, status);      // K is consumed; so are V and P^T of the tile before
             if (PAGES) load_pages(&tm_v, sV, bar_vfull, cur);
-            if (it + 1 < my_tiles) load_k(it + 1, nxt);
+            if (it + 1 < my_tiles) load_k(nxt);
+            const bool first = cur.first;
             cur = nxt;
-            fetch_ids(it + 2, nxt);
+            fetch(nxt);
             mbar_wait(bar_p, it & 1, abort_flag, status);
             if (PAGES) mbar_wait(bar_vfull, it & 1, abort_flag, status);
             tc_fence_after();
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {               // O^T += V^T P^T, 16 keys per step
                 const uint64_t offp = (uint64_t)(((kk >> 2) * QBOX + (kk & 3) * 32) >> 4);
-                if (leader) mma_ss(tmem_O, dV + (uint64_t)(kk * 128), dP + offp, IDESC_O, (it > 0) || (kk > 0));
+                if (leader) mma_ss(tmem_O, dV + (uint64_t)(kk * 128), dP + offp, IDESC_O, !first || (kk > 0));
             }
             if (leader) mma_commit(bar_done);
         }
     } else {
         // ================= softmax warps =================
         const uint32_t lane_sel = (uint32_t)(warp * 32) << 16;
+        WindowCursor c = start;
         float l_part[COLS];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) l_part[c] = 0.f;
+        for (int i = 0; i < COLS; ++i) l_part[i] = 0.f;
         auto sees = [&](int j, int at) { return j <= at && (j < p.sinks || at - j < p.window); };
         // WIN_ROWS: this thread's rows of a tile's V (16 bytes of every RPI-th), the block-table entries one tile ahead; rows that no query
         // sees are filled with zeros
         constexpr int LPR = D / 8, RPI = 32 / LPR, NIT = PAGES ? 1 : 32 / RPI;
         int pid[NIT];
         auto row_of = [&](int j) { return warp * 32 + j * RPI + lane / LPR; };
-        auto fetch_pids = [&](int i) {
+        auto fetch_pids = [&](const WindowCursor& at) {
             if constexpr (!PAGES) {
-                if (i >= my_tiles) return;
+                const int32_t* bt = p.block_table + (size_t)at.u.s * p.max_pages;
 #pragma unroll
                 for (int j = 0; j < NIT; ++j) {
                     int en, o;
-                    split_token(min(tile_at(i) * 128 + row_of(j), end - 1), en, o);
+                    split_token(min(at.u.key_of(at.i) + row_of(j), at.u.end - 1), en, o);
                     pid[j] = bt[en];
                 }
             }
         };
         auto load_v_rows = [&](int k0) {
-            const int c = lane % LPR;
+            const int l = lane % LPR;
 #pragma unroll
             for (int j = 0; j < NIT; ++j) {
                 const int r = row_of(j);
                 int en, o;
-                split_token(min(k0 + r, end - 1), en, o);
+                split_token(min(k0 + r, c.u.end - 1), en, o);
                 const size_t row = (size_t)checked_page(pid[j]) * ps + o;
-                const uint32_t dst = (uint32_t)((c >> 3) * BOX + r * 128 + (((c & 7) ^ (r & 7)) << 4)), bytes = seen_by_some(k0 + r) ? 16u : 0u;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sV + dst), "l"(p.v_cache + (row * p.Hkv + g) * D + c * 8), "r"(bytes)
+                const uint32_t dst = (uint32_t)((l >> 3) * BOX + r * 128 + (((l & 7) ^ (r & 7)) << 4)), bytes = c.u.seen_by_some(k0 + r) ? 16u : 0u;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sV + dst), "l"(p.v_cache + (row * p.Hkv + c.g) * D + l * 8), "r"(bytes)
                              : "memory");
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         // O^T += weight x V for the rows of the tile at k0 that were kept out of the second product.  O^T is up to date, P^T still there.
+        const int* at_of = s_at;              // of the columns of the head in work
         auto patch = [&](int k0) {
+            const int32_t* bt = p.block_table + (size_t)c.u.s * p.max_pages;
+            const int cols = c.u.cols;
             for (int r0 = 0; r0 < 128; r0 += 32)
                 for (uint32_t m = s_bad[r0 >> 5]; m; m &= m - 1) {
                     const int r = r0 + __ffs(m) - 1;
                     int en, o;
                     split_token(k0 + r, en, o);
                     const size_t row = (size_t)checked_page(bt[en]) * ps + o;
-                    const float v = __bfloat162float(p.v_cache[(row * p.Hkv + g) * D + tid % D]);
+                    const float v = __bfloat162float(p.v_cache[(row * p.Hkv + c.g) * D + tid % D]);
                     for (int c0 = 0; c0 < cols; c0 += 16) {
                         uint32_t x[16];
                         tmem_ld16(tmem_O + c0 + lane_sel, x);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int c = 0; c < 16; ++c)
-                            if (sees(k0 + r, s_at[c0 + c])) {
-                                const uint8_t* w = sgen + SM::OFF_P + (r >> 6) * QBOX + (c0 + c) * 128 + ((((r & 63) >> 3) ^ (c & 7)) << 4) + ((r & 7) << 1);
-                                x[c] = __float_as_uint(__uint_as_float(x[c]) + __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(w)) * v);
+                        for (int i = 0; i < 16; ++i)
+                            if (sees(k0 + r, at_of[c0 + i])) {
+                                const uint8_t* w = sgen + SM::OFF_P + (r >> 6) * QBOX + (c0 + i) * 128 + ((((r & 63) >> 3) ^ (i & 7)) << 4) + ((r & 7) << 1);
+                                x[i] = __float_as_uint(__uint_as_float(x[i]) + __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(w)) * v);
                             }
                         tmem_st16(tmem_O + c0 + lane_sel, x);
                         tmem_wait_st();
                     }
                 }
         };
+        // the queries of the head at the cursor, columns' positions and rows in half `which`
+        auto load_q = [&](int which) {
+            if (tid < COLS) {
+                const int t = tid / G;
+                s_at[which * COLS + tid] = tid < c.u.cols ? c.u.at0 + t : -1;
+                s_row[which * COLS + tid] = tid < c.u.cols ? (c.u.s * p.n_new + c.u.tok0 + t) * p.Hq + c.g * G + (tid - t * G) : -1;
+            }
+            named_bar_sync(1, 128);
+            // column, 16-byte chunk of its row: box, then chunk ^ (column % 8) of the 128-byte row; columns past the last are zero
+            constexpr int NQ = COLS * (D / 8) / 128;         // chunks a thread, all on their way before the first is stored
+            uint4 v[NQ];
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) {
+                const int i = tid + k * 128, row = s_row[which * COLS + i / (D / 8)];
+                v[k] = row >= 0 ? *reinterpret_cast<const uint4*>(p.q + (size_t)row * D + (i % (D / 8)) * 8) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) {
+                const int i = tid + k * 128, col = i / (D / 8), c16 = i % (D / 8);
+                *reinterpret_cast<uint4*>(sgen + SM::OFF_Q + (c16 >> 3) * QBOX + col * 128 + (((c16 & 7) ^ (col & 7)) << 4)) = v[k];
+            }
+            fence_proxy_async();
+            mbar_arrive(bar_q);
+        };
+        load_q(0);
+        fetch_pids(c);
         bool to_patch = false;
-        fetch_pids(0);
+        int before_k0 = 0, left = my_tiles, which = 0;
+        bool first = true;                                      // of the head's tiles in this CTA
         for (int it = 0; it < my_tiles; ++it) {
-            const int k0 = tile_at(it) * 128, j = k0 + tid;
+            const WindowUnit& u = c.u;
+            const int k0 = u.key_of(c.i), j = k0 + tid, cols = u.cols, at0 = u.at0, end = u.end;
+            at_of = s_at + which * COLS;
+            const bool last = --left == 0 || c.i + 1 == u.tiles;
             mbar_wait(bar_s, it & 1, abort_flag, status);       // S^T ready; V, P^T free; O^T up to date
             tc_fence_after();
             if (to_patch) {                                     // the same decision in every thread
-                patch(tile_at(it - 1) * 128);
+                patch(before_k0);
                 named_bar_sync(1, 128);                         // P^T is written again below
             }
             if (!PAGES) {
                 load_v_rows(k0);
-                fetch_pids(it + 1);
+                if (!last) {
+                    ++c.i;
+                    fetch_pids(c);
+                    --c.i;
+                }
             }
             // some query does not see some key of the tile
             const bool masked = k0 + 127 > at0 || !(k0 + 127 < p.sinks || end - 1 - k0 < p.window);
@@ -349,7 +468,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     tmem_ld16(tmem_S + c0 + lane_sel, r);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) sc[c0 + c] = __uint_as_float(r[c]) * p.scale_log2;
+                    for (int x = 0; x < 16; ++x) sc[c0 + x] = __uint_as_float(r[x]) * p.scale_log2;
                 }
             // in blocks of 8 columns, without a branch inside, so that a block's loads and exponentials overlap
             if (masked) {
@@ -357,7 +476,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 for (int c0 = 0; c0 < COLS; c0 += 8)
                     if (c0 < cols) {
 #pragma unroll
-                        for (int c = c0; c < c0 + 8; ++c) sc[c] = sees(j, s_at[c]) ? sc[c] : -INFINITY;
+                        for (int x = c0; x < c0 + 8; ++x) sc[x] = sees(j, at_of[x]) ? sc[x] : -INFINITY;
                     }
             }
             bool above = false;
@@ -367,7 +486,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     const float4 a = *reinterpret_cast<const float4*>(s_ref + c0), b = *reinterpret_cast<const float4*>(s_ref + c0 + 4);
                     const float ref[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) above |= sc[c0 + c] - ref[c] > 8.0f;
+                    for (int x = 0; x < 8; ++x) above |= sc[c0 + x] - ref[x] > 8.0f;
                 }
             if (group_any(1, 128, above)) {
                 // the columns' maxima over the tile; the references that are too low move there
@@ -375,9 +494,9 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 for (int c0 = 0; c0 < COLS; c0 += 8)
                     if (c0 < cols) {
 #pragma unroll
-                        for (int c = c0; c < c0 + 8; ++c) {
-                            const int m = __reduce_max_sync(0xffffffffu, window_order(sc[c]));
-                            if (lane == 0) s_wmax[warp * COLS + c] = window_unorder(m);
+                        for (int x = c0; x < c0 + 8; ++x) {
+                            const int m = __reduce_max_sync(0xffffffffu, window_order(sc[x]));
+                            if (lane == 0) s_wmax[warp * COLS + x] = window_unorder(m);
                         }
                     }
                 named_bar_sync(1, 128);
@@ -392,15 +511,15 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 for (int c0 = 0; c0 < COLS; c0 += 8)
                     if (c0 < cols) {
 #pragma unroll
-                        for (int c = c0; c < c0 + 8; ++c) l_part[c] *= c < cols ? s_alpha[c] : 1.f;
+                        for (int x = c0; x < c0 + 8; ++x) l_part[x] *= x < cols ? s_alpha[x] : 1.f;
                     }
-                if (it > 0) {                     // O^T row d = tid
+                if (!first) {                     // O^T row d = tid
                     for (int c0 = 0; c0 < cols; c0 += 16) {
                         uint32_t o[16];
                         tmem_ld16(tmem_O + c0 + lane_sel, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * (c0 + c < cols ? s_alpha[c0 + c] : 0.f));
+                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * (c0 + x < cols ? s_alpha[c0 + x] : 0.f));
                         tmem_st16(tmem_O + c0 + lane_sel, o);
                         tmem_wait_st();
                     }
@@ -415,10 +534,10 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     const float4 a = *reinterpret_cast<const float4*>(s_ref + c0), b = *reinterpret_cast<const float4*>(s_ref + c0 + 4);
                     const float ref[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float w = fast_exp2(sc[c0 + c] - ref[c]);
-                        l_part[c0 + c] += w;
-                        *reinterpret_cast<__nv_bfloat16*>(prow + (c0 + c) * 128 + ((chunk ^ c) << 4)) = __float2bfloat16(w);
+                    for (int x = 0; x < 8; ++x) {
+                        const float w = fast_exp2(sc[c0 + x] - ref[x]);
+                        l_part[c0 + x] += w;
+                        *reinterpret_cast<__nv_bfloat16*>(prow + (c0 + x) * 128 + ((chunk ^ x) << 4)) = __float2bfloat16(w);
                     }
                 }
             if (!PAGES) asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -426,7 +545,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             if (masked) {                         // the same decision in every thread
                 if (PAGES) mbar_wait(bar_vfull, it & 1, abort_flag, status);
                 else named_bar_sync(1, 128);      // other threads fetched this thread's row
-                bool clear = !seen_by_some(j), bad = false;
+                bool clear = !u.seen_by_some(j), bad = false;
                 uint4* vrow = reinterpret_cast<uint4*>(sgen + SM::OFF_V + tid * 128);
                 if (!clear && !(sees(j, at0) && sees(j, end - 1))) {
                     // some see it and others do not (or may not): it has to be finite
@@ -453,56 +572,76 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             fence_proxy_async();      // P^T and the V rows written by this thread visible to the tensor core's reads of shared memory
             tc_fence_before();
             mbar_arrive(bar_p);
-        }
-        // ---- this split's partial result: O^T (unnormalised), the references and the sums ----
-        if (my_tiles > 0) {
-            mbar_wait(bar_done, (my_tiles - 1) & 1, abort_flag, status);
-            tc_fence_after();
-            if (to_patch) patch(tile_at(my_tiles - 1) * 128);
-        }
-        // sums of 8 columns over the warp's lanes: the lanes halve the columns that they hold three times, then add twice
-#pragma unroll
-        for (int c0 = 0; c0 < COLS; c0 += 8)
-            if (c0 < cols) {
-                float v[8];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) v[c] = l_part[c0 + c];
-#pragma unroll
-                for (int half = 4; half > 0; half >>= 1) {
-                    const bool upper = lane & (half * 4);
-#pragma unroll
-                    for (int c = 0; c < half; ++c) {
-                        const float mine = upper ? v[c + half] : v[c], other = upper ? v[c] : v[c + half];
-                        v[c] = mine + __shfl_xor_sync(0xffffffffu, other, half * 4);
-                    }
-                }
-                v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
-                v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
-                if ((lane & 3) == 0) s_wmax[warp * COLS + c0 + (lane >> 2)] = v[0];
+            first = last;
+            if (!last) {
+                before_k0 = k0;
+                ++c.i;
+                continue;
             }
-        for (int c0 = 0; c0 < cols; c0 += 16) {
-            uint32_t o[16];
-            if (my_tiles > 0) {
+            // ---- the head's part is done.  Its result's place first, then the next head's queries (K is there already) ----
+            const int part = (int)(blockIdx.x - (c.before * p.Hkv + (long long)c.g * u.tiles) / share);
+            const int result = which * COLS;
+            const WindowCursor done = c;
+            if (left > 0) {
+                c.next_unit(p);
+                which ^= 1;
+                load_q(which);
+                fetch_pids(c);
+            }
+            mbar_wait(bar_done, it & 1, abort_flag, status);
+            tc_fence_after();
+            if (to_patch) {
+                const WindowCursor next = c;
+                c = done;
+                patch(k0);
+                c = next;
+                to_patch = false;
+            }
+            // sums of 8 columns over the warp's lanes: the lanes halve the columns that they hold three times, then add twice
+#pragma unroll
+            for (int c0 = 0; c0 < COLS; c0 += 8)
+                if (c0 < cols) {
+                    float v[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) v[x] = l_part[c0 + x];
+#pragma unroll
+                    for (int half = 4; half > 0; half >>= 1) {
+                        const bool upper = lane & (half * 4);
+#pragma unroll
+                        for (int x = 0; x < half; ++x) {
+                            const float mine = upper ? v[x + half] : v[x], other = upper ? v[x] : v[x + half];
+                            v[x] = mine + __shfl_xor_sync(0xffffffffu, other, half * 4);
+                        }
+                    }
+                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
+                    if ((lane & 3) == 0) s_wmax[warp * COLS + c0 + (lane >> 2)] = v[0];
+                }
+            for (int c0 = 0; c0 < cols; c0 += 16) {
+                uint32_t o[16];
                 tmem_ld16(tmem_O + c0 + lane_sel, o);
                 tmem_wait_ld();
-            } else {
+                if (tid < D) {
 #pragma unroll
-                for (int c = 0; c < 16; ++c) o[c] = 0u;
-            }
-            if (tid < D) {
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const int row = s_row[c0 + c];
-                    if (row >= 0) p.part_o[((size_t)row * p.nsplit + z) * D + tid] = __uint_as_float(o[c]);
+                    for (int x = 0; x < 16; ++x) {
+                        const int row = s_row[result + c0 + x];
+                        if (row >= 0) p.part_o[((size_t)row * p.nsplit + part) * D + tid] = __uint_as_float(o[x]);
+                    }
                 }
             }
-        }
-        named_bar_sync(1, 128);
-        if (tid < cols) {
-            const float ref = s_ref[tid];
-            float* ml = p.part_ml + ((size_t)s_row[tid] * p.nsplit + z) * 2;
-            ml[0] = ref == WIN_UNSET ? -INFINITY : ref;
-            ml[1] = flagged_sum(s_wmax[tid] + s_wmax[COLS + tid] + s_wmax[2 * COLS + tid] + s_wmax[3 * COLS + tid], *(volatile int32_t*)status);
+            named_bar_sync(1, 128);
+            if (tid < cols) {
+                const float ref = s_ref[tid];
+                float* ml = p.part_ml + ((size_t)s_row[result + tid] * p.nsplit + part) * 2;
+                ml[0] = ref == WIN_UNSET ? -INFINITY : ref;
+                ml[1] = flagged_sum(s_wmax[tid] + s_wmax[COLS + tid] + s_wmax[2 * COLS + tid] + s_wmax[3 * COLS + tid], *(volatile int32_t*)status);
+            }
+            if (left > 0) {
+                if (tid < COLS) s_ref[tid] = tid < c.u.cols ? WIN_UNSET : 0.f;
+#pragma unroll
+                for (int x = 0; x < COLS; ++x) l_part[x] = 0.f;
+                named_bar_sync(1, 128);                         // the references are read by all
+            }
         }
     }
     tc_fence_before();
@@ -511,6 +650,20 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         __syncwarp();
         tmem_dealloc(tmem_S, 2 * COLS);
     }
+}
+
+// A warp for a row (sequence, token, query head): its head's tiles began in CTA `first` and went on for `count`
+template <int D, int PART>
+__global__ void __launch_bounds__(256) window_merge_kernel(MergeParams m, const WindowEntry* entries, int Hq, int G, int Hkv, int n_new, int groups,
+                                                          int group_tokens) {
+    pdl_wait();
+    const int row = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    if (row >= m.rows) return;
+    const int token = row / Hq, g = (row - token * Hq) / G, s = token / n_new;
+    const WindowEntry e = entries[s * groups + (token - s * n_new) / group_tokens];
+    const long long share = *reinterpret_cast<const long long*>(m.header + WIN_SHARE_WORD), at = e.before * Hkv + (long long)g * e.tiles;
+    const int count = e.tiles == 0 ? 0 : (int)((at + e.tiles - 1) / share - at / share + 1);
+    decode_merge_row<D, PART>(m, row, threadIdx.x & 31, count);
 }
 
 }  // namespace kvs
@@ -531,27 +684,44 @@ int window_groups(int G, int n_new) {
 }
 
 template <int D, int COLS>
-int launch_window(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, bool pages, cudaStream_t st) {
+int launch_window(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, long long most_tiles, bool pages, cudaStream_t st) {
     auto kern = pages ? decode_window_kernel<D, COLS, WIN_PAGES> : decode_window_kernel<D, COLS, WIN_ROWS>;
-    constexpr int bytes = WinSmem<D, COLS>::DYN_BYTES;
+    constexpr int bytes = WinSmem<D, COLS>::DYN_BYTES, resident = WinSmem<D, COLS>::CTAS;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return cuda_refused();
-    return launch_after(kern, dim3((unsigned)p.nsplit, (unsigned)p.Hkv, (unsigned)(p.S * p.groups)), WIN_THREADS, bytes, st, tk, tv, p);
+    const long long ctas = most_tiles < 148 * resident ? most_tiles : 148 * resident;        // one wave
+    return launch_after(kern, dim3((unsigned)(ctas < 1 ? 1 : ctas)), WIN_THREADS, bytes, st, tk, tv, p);
 }
 template <int D>
-int launch_window_cols(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, bool pages, cudaStream_t st) {
+int launch_window_cols(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, const MergeParams& m, long long most_tiles, bool pages,
+                       cudaStream_t st) {
     const int cols = p.G * p.group_tokens;
-    if (cols <= 16) return launch_window<D, 16>(tk, tv, p, pages, st);
-    if (cols <= 32) return launch_window<D, 32>(tk, tv, p, pages, st);
-    return launch_window<D, 64>(tk, tv, p, pages, st);
+    const int rc = cols <= 16 ? launch_window<D, 16>(tk, tv, p, most_tiles, pages, st)
+                 : cols <= 32 ? launch_window<D, 32>(tk, tv, p, most_tiles, pages, st)
+                              : launch_window<D, 64>(tk, tv, p, most_tiles, pages, st);
+    if (rc != KVS_OK) return rc;
+    return launch_after(p.nsplit <= 4 ? window_merge_kernel<D, 4> : window_merge_kernel<D, 16>, (unsigned)((m.rows + 7) / 8), 256, 0, st, m, p.entries, p.Hq,
+                        p.G, p.Hkv, p.n_new, p.groups, p.group_tokens);
+}
+// rows' results, room for one part more than num_splits (a border may fall anywhere in a head's tiles); then the entries
+size_t window_entries_offset(int num_seqs, int n_new, int Hq, int head_dim, int num_splits) {
+    return DEC_WS_HEADER + align_up(sizeof(float) * (size_t)num_seqs * n_new * Hq * ((size_t)num_splits + 1) * (head_dim + 2), 256);
 }
 }  // namespace
 
 extern "C" int kvs_decode_window_num_splits(int num_seqs, int n_new, int Hq, int Hkv, int max_tokens, int window, int sinks) {
     if (num_seqs <= 0 || n_new <= 0 || Hq <= 0 || Hkv <= 0 || max_tokens <= 0 || window <= 0 || sinks < 0) return 1;
     if (Hq % Hkv != 0 || Hq / Hkv > WIN_MOST_COLS) return 1;
-    const long long tiles = window_tiles(n_new, max_tokens, window, sinks);
-    const long long seqs = (long long)num_seqs * window_groups(Hq / Hkv, n_new);
-    return kvs_decode_num_splits((int)(seqs < 65535 ? seqs : 65535), Hkv, (int)(tiles * 128 < 0x7fffffff ? tiles * 128 : 0x7fffffff));
+    // every CTA of a wave of three an SM has an equal share; a sequence four times as long as the mean is still cut as small as that
+    const long long units = (long long)num_seqs * window_groups(Hq / Hkv, n_new) * Hkv, tiles = window_tiles(n_new, max_tokens, window, sinks);
+    long long n = (4 * 3 * 148 + units - 1) / units;
+    if (n > tiles) n = tiles;
+    return (int)(n > 64 ? 64 : n < 1 ? 1 : n);
+}
+
+extern "C" size_t kvs_decode_window_workspace_bytes(int num_seqs, int n_new, int Hq, int Hkv, int head_dim, int num_splits) {
+    if (num_seqs < 0 || n_new < 0 || Hq <= 0 || Hkv <= 0 || head_dim <= 0 || num_splits <= 0) return 0;
+    if (Hq % Hkv != 0 || Hq / Hkv > WIN_MOST_COLS) return 0;
+    return window_entries_offset(num_seqs, n_new, Hq, head_dim, num_splits) + sizeof(WindowEntry) * (size_t)num_seqs * window_groups(Hq / Hkv, n_new);
 }
 
 extern "C" int kvs_decode_attn_window(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table, const int32_t* n_tokens,
@@ -562,17 +732,17 @@ extern "C" int kvs_decode_attn_window(const void* q, const void* k_cache, const 
         return KVS_ERR_INVALID_ARG;
     if (softmax_scale < 0.f || softmax_scale != softmax_scale) return KVS_ERR_INVALID_ARG;
     if (head_dim != 64 && head_dim != 128) return KVS_ERR_UNSUPPORTED;
-    if (Hq % Hkv != 0 || Hkv > 65535 || Hq / Hkv > WIN_MOST_COLS) return KVS_ERR_UNSUPPORTED;
+    if (Hq % Hkv != 0 || Hq / Hkv > WIN_MOST_COLS) return KVS_ERR_UNSUPPORTED;
     if (num_seqs == 0 || n_new == 0) return KVS_OK;
     const int G = Hq / Hkv, groups = window_groups(G, n_new);
-    if ((long long)num_seqs * groups > 65535 || (long long)num_seqs * n_new * Hq > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
+    if ((long long)num_seqs * groups > 0x7fffffffLL || (long long)num_seqs * n_new * Hq > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
     if ((long long)num_pages * page_size > 0x7fffffffLL || (long long)max_pages * page_size > 0x7fffff00LL || (long long)Hkv * head_dim > 0x7fffffffLL)
         return KVS_ERR_UNSUPPORTED;
     if (!q || !k_cache || !v_cache || !block_table || !n_tokens || !out || !lse || !workspace) return KVS_ERR_INVALID_ARG;
     if ((((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) & 15) != 0 || ((uintptr_t)workspace & 255) != 0 ||
         (((uintptr_t)block_table | (uintptr_t)n_tokens | (uintptr_t)lse) & 3) != 0)
         return KVS_ERR_ALIGNMENT;
-    if (workspace_bytes < kvs_decode_workspace_bytes(num_seqs * n_new, Hq, head_dim, num_splits)) return KVS_ERR_WORKSPACE;
+    if (workspace_bytes < kvs_decode_window_workspace_bytes(num_seqs, n_new, Hq, Hkv, head_dim, num_splits)) return KVS_ERR_WORKSPACE;
     int rc = check_device_sm100();
     if (rc != KVS_OK) return rc;
     WindowParams p;
@@ -589,7 +759,7 @@ extern "C" int kvs_decode_attn_window(const void* q, const void* k_cache, const 
     p.page_shift = (page_size & (page_size - 1)) == 0 ? __builtin_ctz((unsigned)page_size) : -1;
     p.max_pages = max_pages;
     p.num_pages = num_pages;
-    p.nsplit = num_splits;
+    p.nsplit = num_splits + 1;
     p.groups = groups;
     p.group_tokens = (n_new + groups - 1) / groups;
     p.window = window;
@@ -597,7 +767,8 @@ extern "C" int kvs_decode_attn_window(const void* q, const void* k_cache, const 
     p.header = (int32_t*)workspace;
     p.scale_log2 = (softmax_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : softmax_scale) * 1.4426950408889634f;
     p.part_o = (float*)((char*)workspace + DEC_WS_HEADER);
-    p.part_ml = p.part_o + (size_t)num_seqs * n_new * Hq * num_splits * head_dim;
+    p.part_ml = p.part_o + (size_t)num_seqs * n_new * Hq * p.nsplit * head_dim;
+    p.entries = (WindowEntry*)((char*)workspace + window_entries_offset(num_seqs, n_new, Hq, head_dim, num_splits));
     // pages that are whole 8-row swizzle atoms and tile 128 tokens come by one TMA box each; no box reaches past the cache
     const bool pages = page_size % 8 == 0 && page_size <= 128 && 128 % page_size == 0;
     CUtensorMap tk, tv;
@@ -610,8 +781,7 @@ extern "C" int kvs_decode_attn_window(const void* q, const void* k_cache, const 
         if ((rc = make_tmap_rows(&tk, k_cache, num_pages * page_size, Hkv * head_dim)) != KVS_OK) return rc;
     }
     cudaStream_t st = (cudaStream_t)stream;
-    rc = head_dim == 64 ? launch_window_cols<64>(tk, tv, p, pages, st) : launch_window_cols<128>(tk, tv, p, pages, st);
-    if (rc != KVS_OK) return rc;
-    const MergeParams m = {p.part_o, p.part_ml, (__nv_bfloat16*)out, lse, p.header, num_seqs * n_new * Hq, num_splits};
-    return launch_decode_merge(m, head_dim, st);
+    const MergeParams m = {p.part_o, p.part_ml, (__nv_bfloat16*)out, lse, p.header, num_seqs * n_new * Hq, p.nsplit};
+    const long long most_tiles = window_tiles(n_new, max_pages * page_size, window, sinks) * num_seqs * groups * Hkv;
+    return head_dim == 64 ? launch_window_cols<64>(tk, tv, p, m, most_tiles, pages, st) : launch_window_cols<128>(tk, tv, p, m, most_tiles, pages, st);
 }

@@ -123,7 +123,7 @@ def test_host_refusals_need_no_gpu(lib):
     assert window(S=-1) == window(new=-1) == window(Hq=0) == window(Hkv=0) == window(page=0) == window(P=0) == window(pool=0) == B.KVS_ERR_INVALID_ARG
     assert window(w=0) == window(sinks=-1) == window(splits=0) == window(scale=-1.0) == window(scale=float("nan")) == window(q=None) == B.KVS_ERR_INVALID_ARG
     assert window(d=96) == window(Hq=5) == window(Hq=130) == window(page=1 << 16, pool=1 << 16) == window(page=1 << 16, P=1 << 16) == B.KVS_ERR_UNSUPPORTED
-    assert window(S=70000) == window(new=1 << 29) == B.KVS_ERR_UNSUPPORTED
+    assert window(S=1 << 30) == window(new=1 << 29) == B.KVS_ERR_UNSUPPORTED
     assert window(q=p + 8) == window(ws=p + 128) == B.KVS_ERR_ALIGNMENT and window(room=256) == B.KVS_ERR_WORKSPACE
     assert window(S=0, q=None) == window(new=0) == B.KVS_OK
 
