@@ -5,9 +5,10 @@
 // products run on the tensor core in the transposed form, so that a tile's 128 keys fill its 128 rows and the few queries its columns:
 //   S^T [128 keys x N] = K [128 x d] Q^T            A = K tile, B = Q: column c is query head c % G of token c / G
 //   O^T [d x N]       += V^T [d x 128 keys] P^T     A = V tile read MN-major, B = P^T  (d = 64: rows 64 .. 127 repeat rows 0 .. 63)
-// Four softmax warps (a thread has a key of S^T and a column d of O^T) and a control warp (block table, TMA loads, MMA issue).  K of
-// tile t + 1 is asked for as soon as S^T of tile t is complete, V of tile t as soon as the second product of tile t - 1 is; two or three
-// CTAs an SM overlap one another's loads, products and softmax.
+// Four softmax warps (a thread has a key of S^T and a column d of O^T; from 17 columns on eight, which halve the columns), a warp that
+// issues the products, one that loads K and two that load V (by one control warp a tile took 5900 clocks, 1300 of them to issue its 16 TMA
+// instructions for K, as many for V).  S^T of tile t + 1 is formed while tile t is in work, K of tile t + 2 is asked for as soon as
+// that is complete, V of tile t + 1 as soon as the second product of tile t is; two or three CTAs an SM overlap what is left of the chain.
 //
 // Every CTA has an equal share of all tiles: the tiles of (sequence and group of new tokens, KV head) follow one another, CTA c has
 // tiles c share .. (c + 1) share - 1 of them, whose heads end where they end.  Lengths are ragged and known on the device alone, so every
@@ -29,7 +30,6 @@
 
 namespace kvs {
 
-constexpr int WIN_THREADS = 160;
 constexpr int WIN_PAGES = 1;         // one TMA box per page
 constexpr int WIN_ROWS = 2;          // K: TMA gather4; V: cp.async rows
 constexpr float WIN_UNSET = -1e30f;  // reference of a column that has seen no key yet: any score is far above it
@@ -98,7 +98,11 @@ struct WindowCursor {
 
 template <int D, int COLS>
 struct WinSmem {
-    static constexpr int CTAS = COLS <= 16 || (COLS <= 32 && D == 64) ? 3 : 2;      // an SM
+    static constexpr int HALVES = COLS >= 32 ? 2 : 1;                  // threads that share a key's columns
+    static constexpr int WORKERS = 128 * HALVES, THREADS = WORKERS + 128;
+    static constexpr int CTAS = COLS <= 16 ? 3 : 2;                    // an SM: 24 warps, 80 registers a thread at launch ...
+    static constexpr int WORKER_REGS = COLS <= 16 ? 104 : 96, CONTROL_REGS = COLS <= 16 ? 56 : 48;      // ... and shared out among the warp groups like this
+    static_assert(WORKERS * WORKER_REGS + 128 * CONTROL_REGS <= THREADS * 80, "no more than the block was launched with");
     static constexpr int TILE_BYTES = 128 * D * 2;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_V = TILE_BYTES;
@@ -135,10 +139,13 @@ __device__ __forceinline__ bool group_any(int id, int nthreads, bool mine) {
 }
 
 template <int D, int COLS, int LOAD>
-__global__ void __launch_bounds__(WIN_THREADS, WinSmem<D, COLS>::CTAS)
+__global__ void __launch_bounds__(WinSmem<D, COLS>::THREADS, WinSmem<D, COLS>::CTAS)
 decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ WindowParams p) {
     using SM = WinSmem<D, COLS>;
     constexpr int BOX = 16384, NBOX = D / 64;
+    constexpr int WORKERS = SM::WORKERS, THREADS = SM::THREADS, CONTROL = WORKERS / 32;        // CONTROL: the first control warp
+    constexpr int WIDE = COLS / SM::HALVES;              // columns of a thread
+    constexpr int CH = COLS <= 16 ? 8 : 16;              // of which it holds the scores at a time
     constexpr int QBOX = COLS * 128;                     // bytes of a 64-wide box of Q or P^T
     constexpr uint32_t IDESC_S = make_idesc(COLS, 0, 0), IDESC_O = make_idesc(COLS, 1, 0);
     constexpr bool PAGES = LOAD == WIN_PAGES;
@@ -156,7 +163,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         long long sum = 0;
         int most = 0;
         WindowUnit u;
-        for (int e = tid; e < E; e += WIN_THREADS) {
+        for (int e = tid; e < E; e += THREADS) {
             u.load(p, e);
             sum += u.tiles;
             most = max(most, u.tiles);
@@ -175,7 +182,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         }
         if (at >= all && blockIdx.x != 0) return;          // the same in the whole CTA
         long long run = 0, here;
-        for (int e0 = 0; e0 < E && (blockIdx.x == 0 || run * p.Hkv <= at); e0 += WIN_THREADS) {
+        for (int e0 = 0; e0 < E && (blockIdx.x == 0 || run * p.Hkv <= at); e0 += THREADS) {
             const int e = e0 + tid;
             u.tiles = 0;
             if (e < E) u.load(p, e);
@@ -204,9 +211,9 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     const uint32_t sraw = smem_u32(smem_raw), sbase = (sraw + 1023u) & ~1023u;
     uint8_t* sgen = smem_raw + (sbase - sraw);
     const uint32_t sK = sbase + SM::OFF_K, sV = sbase + SM::OFF_V, sQ = sbase + SM::OFF_Q, sP = sbase + SM::OFF_P, bars = sbase + SM::OFF_BAR;
-    // as in the decode kernel: K / V rows have landed, S^T complete (hence K, and the V and P^T of the tile before, consumed), P^T
-    // written, second product complete; and the queries of a head are in place
-    const uint32_t bar_kfull = bars, bar_vfull = bars + 8, bar_s = bars + 16, bar_p = bars + 24, bar_done = bars + 32, bar_q = bars + 40;
+    // K / V rows have landed; S^T is complete (one for each of its two buffers: the one of tile t + 2 waits for P^T of tile t, that of
+    // t + 1 does not); P^T is written; the second product is complete (V and P^T consumed, O^T up to date); a head's queries are in place
+    const uint32_t bar_kfull = bars, bar_vfull = bars + 8, bar_s = bars + 16, bar_p = bars + 32, bar_done = bars + 40, bar_q = bars + 48;
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(sgen + SM::OFF_MISC);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + SM::OFF_MISC + 4);
     int32_t* status = reinterpret_cast<int32_t*>(sgen + SM::OFF_MISC + 8);
@@ -221,15 +228,16 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         *abort_flag = 0;
         *status = KVS_OK;
         mbar_init(bar_kfull, 1);
-        mbar_init(bar_vfull, 1);
+        mbar_init(bar_vfull, PAGES ? 2 : 64);
         mbar_init(bar_s, 1);
-        mbar_init(bar_p, 128);
+        mbar_init(bar_s + 8, 1);
+        mbar_init(bar_p, WORKERS);
         mbar_init(bar_done, 1);
-        mbar_init(bar_q, 128);
+        mbar_init(bar_q, WORKERS);
         fence_mbar_init();
     }
-    if (warp == 4) {
-        tmem_alloc(smem_u32(s_tmem), 2 * COLS);
+    if (warp == CONTROL) {
+        tmem_alloc(smem_u32(s_tmem), 4 * COLS);            // S^T twice and O^T, in a power of two
         tmem_relinquish();
     } else if (tid < COLS) {
         s_ref[tid] = tid < start.u.cols ? WIN_UNSET : 0.f;       // columns past the last score 0 and never move
@@ -237,7 +245,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_S = *s_tmem, tmem_O = tmem_S + COLS;
+    const uint32_t tmem_S = *s_tmem, tmem_O = tmem_S + 2 * COLS;
     auto split_token = [&](int tok, int& entry, int& offset) {
         entry = p.page_shift >= 0 ? tok >> p.page_shift : tok / ps;
         offset = tok - entry * ps;
@@ -249,140 +257,161 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         return 0;
     };
 
-    if (warp == 4) {
-        // ================= control warp: block table, TMA loads, MMA issue =================
+    if (warp >= CONTROL) {
+        // ================= control warps: one issues the products, one loads K, two load V =================
+        reg_dec<SM::CONTROL_REGS>();
         const bool leader = elect_one();
-        const uint64_t dK = smem_desc(sK, 16, 1024), dQ = smem_desc(sQ, 16, 1024);
-        const uint64_t dV = smem_desc(sV, D == 128 ? BOX : 0, 1024), dP = smem_desc(sP, 16, 1024);
         const int ppt = PAGES ? 128 / ps : 0;                  // pages per tile
-        // PAGES: lane i has page i of the tile, if some query sees a row of it; ROWS: lane L the pages of rows 4 L .. 4 L + 3 (rows past the
-        // end repeat the last one: their scores are masked), if some query sees one of them
-        struct Tile { int k0, end, g, v[PAGES ? 1 : 4]; bool need, first; };
         WindowCursor c = start;
-        int left = my_tiles;
-        auto fetch = [&](Tile& t) {                            // the tile at the cursor, which moves on
-            t.need = false;
-            if (left == 0) return;
-            const int32_t* bt = p.block_table + (size_t)c.u.s * p.max_pages;
-            t.k0 = c.u.key_of(c.i);
-            t.end = c.u.end;
-            t.g = c.g;
-            t.first = left == my_tiles || c.i == 0;
-            const int a = t.k0 + lane * (PAGES ? ps : 4), e = min(a + (PAGES ? ps : 4), c.u.end);
-            t.need = (!PAGES || lane < ppt) && a < e && (a < c.u.head || e > c.u.lo);
-            if constexpr (PAGES) {
-                t.v[0] = t.need ? bt[(t.k0 >> 7) * ppt + lane] : 0;
-            } else if (t.need) {
+        if (warp == CONTROL) {
+            const uint64_t dK = smem_desc(sK, 16, 1024), dQ = smem_desc(sQ, 16, 1024);
+            const uint64_t dV = smem_desc(sV, D == 128 ? BOX : 0, 1024), dP = smem_desc(sP, 16, 1024);
+            int heads = 0;
+            auto scores = [&](int it, bool head) {             // S^T of tile `it`; the first of a head waits for its queries
+                if (head) mbar_wait(bar_q, heads++ & 1, abort_flag, status);
+                mbar_wait(bar_kfull, it & 1, abort_flag, status);
+                tc_fence_after();
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    int en, o;
-                    split_token(min(a + j, c.u.end - 1), en, o);
-                    t.v[j] = bt[en];
+                for (int kk = 0; kk < D / 16; ++kk) {          // S^T = K Q^T, 16 elements of d per step
+                    const uint64_t offk = (uint64_t)(((kk >> 2) * BOX + (kk & 3) * 32) >> 4);
+                    const uint64_t offq = (uint64_t)(((kk >> 2) * QBOX + (kk & 3) * 32) >> 4);
+                    if (leader) mma_ss(tmem_S + (it & 1) * COLS, dK + offk, dQ + offq, IDESC_S, kk > 0);
                 }
-            }
-            if (--left > 0) c.next(p);
-        };
-        auto load_pages = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, const Tile& t) {
-            const uint32_t pages = __popc(__ballot_sync(0xffffffffu, t.need));
-            if (leader) mbar_expect_tx(bar, pages * (uint32_t)(ps * D * 2));
-            __syncwarp();
-            if (t.need) {
-                const int row = checked_page(t.v[0]) * ps;
+                if (leader) mma_commit(bar_s + (it & 1) * 8);
+            };
+            scores(0, true);
+            bool first = true;
+            for (int it = 0; it < my_tiles; ++it) {
+                // the next tile's scores while this one's are in work; those of another head behind P^T, as their queries come behind it
+                const bool more = it + 1 < my_tiles;
+                if (more) c.next(p);
+                const bool head = c.i == 0;
+                if (more && !head) scores(it + 1, false);
+                mbar_wait(bar_p, it & 1, abort_flag, status);
+                mbar_wait(bar_vfull, it & 1, abort_flag, status);
+                tc_fence_after();
 #pragma unroll
-                for (int b = 0; b < NBOX; ++b) tma_load_3d(dst + b * BOX + (uint32_t)(lane * ps) * 128u, map, b * 64, t.g, row, bar);
+                for (int kk = 0; kk < 8; ++kk) {               // O^T += V^T P^T, 16 keys per step
+                    const uint64_t offp = (uint64_t)(((kk >> 2) * QBOX + (kk & 3) * 32) >> 4);
+                    if (leader) mma_ss(tmem_O, dV + (uint64_t)(kk * 128), dP + offp, IDESC_O, !first || (kk > 0));
+                }
+                if (leader) mma_commit(bar_done);
+                first = head;
+                if (more && head) scores(it + 1, true);
             }
-        };
-        auto load_k = [&](const Tile& t) {                     // K buffer must be free
-            if constexpr (PAGES) {
-                load_pages(&tm_k, sK, bar_kfull, t);
-            } else {
-                const uint32_t quads = __popc(__ballot_sync(0xffffffffu, t.need));
-                if (leader) mbar_expect_tx(bar_kfull, quads * (uint32_t)(4 * D * 2));
-                __syncwarp();
-                if (t.need) {
-                    int row[4];
+        } else if (PAGES || warp == CONTROL + 1) {
+            // TMA.  PAGES: lane i has page i of the tile, if some query sees a row of it (of V every second page is the other warp's).
+            // ROWS: K alone, lane L has the rows 4 L .. 4 L + 3 (rows past the end repeat the last one: their scores are masked), if some
+            // query sees one of them.  The block-table entries are read a tile ahead.
+            const bool k_rows = warp == CONTROL + 1;
+            const CUtensorMap* map = k_rows ? &tm_k : &tm_v;
+            const uint32_t dst = k_rows ? sK : sV, full = k_rows ? bar_kfull : bar_vfull;
+            const bool mine = !PAGES || (lane < ppt && (k_rows || (lane & 1) == (warp - CONTROL - 2)));
+            int id[PAGES ? 1 : 4], off[PAGES ? 1 : 4], g = 0;
+            bool need = false;
+            auto fetch = [&]() {                               // of the tile at the cursor
+                const int32_t* bt = p.block_table + (size_t)c.u.s * p.max_pages;
+                const int k0 = c.u.key_of(c.i), a = k0 + lane * (PAGES ? ps : 4), e = min(a + (PAGES ? ps : 4), c.u.end);
+                need = mine && a < e && (a < c.u.head || e > c.u.lo);
+                g = c.g;
+                if constexpr (PAGES) {
+                    if (need) id[0] = bt[(k0 >> 7) * ppt + lane];
+                } else if (need) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        int en, o;
-                        split_token(min(t.k0 + 4 * lane + j, t.end - 1), en, o);
-                        row[j] = checked_page(t.v[j]) * ps + o;
+                        int en;
+                        split_token(min(a + j, c.u.end - 1), en, off[j]);
+                        id[j] = bt[en];
                     }
+                }
+            };
+            fetch();
+            for (int it = 0; it < my_tiles; ++it) {
+                // the buffer's last tile is consumed
+                if (it > 0) {
+                    if (k_rows) mbar_wait(bar_s + ((it - 1) & 1) * 8, ((it - 1) >> 1) & 1, abort_flag, status);
+                    else mbar_wait(bar_done, (it - 1) & 1, abort_flag, status);
+                }
+                const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, need));
+                if (leader) mbar_expect_tx(full, boxes * (uint32_t)((PAGES ? ps : 4) * D * 2));
+                __syncwarp();
+                if (need) {
+                    if constexpr (PAGES) {
+                        const int row = checked_page(id[0]) * ps;
 #pragma unroll
-                    for (int b = 0; b < NBOX; ++b)
-                        tma_gather4(sK + b * BOX + (uint32_t)lane * 512u, &tm_k, t.g * D + b * 64, row[0], row[1], row[2], row[3], bar_kfull);
+                        for (int b = 0; b < NBOX; ++b) tma_load_3d(dst + b * BOX + (uint32_t)(lane * ps) * 128u, map, b * 64, g, row, full);
+                    } else {
+                        int row[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) row[j] = checked_page(id[j]) * ps + off[j];
+#pragma unroll
+                        for (int b = 0; b < NBOX; ++b)
+                            tma_gather4(dst + b * BOX + (uint32_t)lane * 512u, map, g * D + b * 64, row[0], row[1], row[2], row[3], full);
+                    }
+                }
+                __syncwarp();
+                if (it + 1 < my_tiles) {
+                    c.next(p);
+                    fetch();
                 }
             }
-        };
-        Tile cur = {}, nxt = {};
-        fetch(cur);
-        fetch(nxt);
-        load_k(cur);
-        int heads = 0;
-        for (int it = 0; it < my_tiles; ++it) {
-            if (cur.first) mbar_wait(bar_q, heads++ & 1, abort_flag, status);
-            mbar_wait(bar_kfull, it & 1, abort_flag, status);
-            tc_fence_after();
+        } else {
+            // V by rows: 16 bytes of a row a lane, LPR lanes a row, two warps; rows that no query sees are filled with zeros.  A lane has the
+            // block-table entries of two of its warp's 64 rows, read a tile ahead, and hands their rows of the cache to the lanes that copy.
+            constexpr int LPR = D / 8, RPW = 32 / LPR, NIT = 64 / RPW;
+            const int part = warp - CONTROL - 2, l = lane % LPR;
+            auto row_of = [&](int i) { return i / RPW * (2 * RPW) + part * RPW + i % RPW; };         // the warp's i-th row in the tile
+            int id[2];
+            auto fetch = [&]() {
+                const int32_t* bt = p.block_table + (size_t)c.u.s * p.max_pages;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {          // S^T = K Q^T, 16 elements of d per step
-                const uint64_t offk = (uint64_t)(((kk >> 2) * BOX + (kk & 3) * 32) >> 4);
-                const uint64_t offq = (uint64_t)(((kk >> 2) * QBOX + (kk & 3) * 32) >> 4);
-                if (leader) mma_ss(tmem_S, dK + offk, dQ + offq, IDESC_S, kk > 0);
-            }
-            if (leader) mma_commit(bar_s);
-            mbar_wait(bar_s, it & 1, abort_flag, status);      // K is consumed; so are V and P^T of the tile before
-            if (PAGES) load_pages(&tm_v, sV, bar_vfull, cur);
-            if (it + 1 < my_tiles) load_k(nxt);
-            const bool first = cur.first;
-            cur = nxt;
-            fetch(nxt);
-            mbar_wait(bar_p, it & 1, abort_flag, status);
-            if (PAGES) mbar_wait(bar_vfull, it & 1, abort_flag, status);
-            tc_fence_after();
+                for (int h = 0; h < 2; ++h) {
+                    int en, o;
+                    split_token(min(c.u.key_of(c.i) + row_of(lane + 32 * h), c.u.end - 1), en, o);
+                    id[h] = bt[en];
+                }
+            };
+            fetch();
+            for (int it = 0; it < my_tiles; ++it) {
+                if (it > 0) mbar_wait(bar_done, (it - 1) & 1, abort_flag, status);
+                const int k0 = c.u.key_of(c.i);
+                int row[2];                                    // of the cache; -1: seen by no query
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {               // O^T += V^T P^T, 16 keys per step
-                const uint64_t offp = (uint64_t)(((kk >> 2) * QBOX + (kk & 3) * 32) >> 4);
-                if (leader) mma_ss(tmem_O, dV + (uint64_t)(kk * 128), dP + offp, IDESC_O, !first || (kk > 0));
+                for (int h = 0; h < 2; ++h) {
+                    const int k = k0 + row_of(lane + 32 * h);
+                    int en, o;
+                    split_token(min(k, c.u.end - 1), en, o);
+                    const int page = checked_page(id[h]);
+                    row[h] = c.u.seen_by_some(k) ? page * ps + o : -1;
+                }
+                const __nv_bfloat16* src = p.v_cache + (size_t)c.g * D + l * 8;
+#pragma unroll
+                for (int j = 0; j < NIT; ++j) {
+                    const int i = j * RPW + lane / LPR, r = row_of(i), from = __shfl_sync(0xffffffffu, row[j * RPW / 32], i & 31);
+                    const uint32_t dst = (uint32_t)((l >> 3) * BOX + r * 128 + (((l & 7) ^ (r & 7)) << 4)), bytes = from >= 0 ? 16u : 0u;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sV + dst), "l"(src + (size_t)max(from, 0) * p.Hkv * D), "r"(bytes)
+                                 : "memory");
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (it + 1 < my_tiles) {
+                    c.next(p);
+                    fetch();
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                fence_proxy_async();                           // the tensor core reads them
+                mbar_arrive(bar_vfull);
             }
-            if (leader) mma_commit(bar_done);
         }
     } else {
         // ================= softmax warps =================
-        const uint32_t lane_sel = (uint32_t)(warp * 32) << 16;
+        reg_inc<SM::WORKER_REGS>();
+        const int key = tid & 127, col0 = tid < 128 ? 0 : WIDE;          // this thread's key of a tile (and column d of O^T), its first column
+        const uint32_t lane_sel = (uint32_t)((warp & 3) * 32) << 16;
         WindowCursor c = start;
-        float l_part[COLS];
+        float l_part[WIDE];
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) l_part[i] = 0.f;
+        for (int i = 0; i < WIDE; ++i) l_part[i] = 0.f;
         auto sees = [&](int j, int at) { return j <= at && (j < p.sinks || at - j < p.window); };
-        // WIN_ROWS: this thread's rows of a tile's V (16 bytes of every RPI-th), the block-table entries one tile ahead; rows that no query
-        // sees are filled with zeros
-        constexpr int LPR = D / 8, RPI = 32 / LPR, NIT = PAGES ? 1 : 32 / RPI;
-        int pid[NIT];
-        auto row_of = [&](int j) { return warp * 32 + j * RPI + lane / LPR; };
-        auto fetch_pids = [&](const WindowCursor& at) {
-            if constexpr (!PAGES) {
-                const int32_t* bt = p.block_table + (size_t)at.u.s * p.max_pages;
-#pragma unroll
-                for (int j = 0; j < NIT; ++j) {
-                    int en, o;
-                    split_token(min(at.u.key_of(at.i) + row_of(j), at.u.end - 1), en, o);
-                    pid[j] = bt[en];
-                }
-            }
-        };
-        auto load_v_rows = [&](int k0) {
-            const int l = lane % LPR;
-#pragma unroll
-            for (int j = 0; j < NIT; ++j) {
-                const int r = row_of(j);
-                int en, o;
-                split_token(min(k0 + r, c.u.end - 1), en, o);
-                const size_t row = (size_t)checked_page(pid[j]) * ps + o;
-                const uint32_t dst = (uint32_t)((l >> 3) * BOX + r * 128 + (((l & 7) ^ (r & 7)) << 4)), bytes = c.u.seen_by_some(k0 + r) ? 16u : 0u;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sV + dst), "l"(p.v_cache + (row * p.Hkv + c.g) * D + l * 8), "r"(bytes)
-                             : "memory");
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
         // O^T += weight x V for the rows of the tile at k0 that were kept out of the second product.  O^T is up to date, P^T still there.
         const int* at_of = s_at;              // of the columns of the head in work
         auto patch = [&](int k0) {
@@ -394,8 +423,8 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     int en, o;
                     split_token(k0 + r, en, o);
                     const size_t row = (size_t)checked_page(bt[en]) * ps + o;
-                    const float v = __bfloat162float(p.v_cache[(row * p.Hkv + c.g) * D + tid % D]);
-                    for (int c0 = 0; c0 < cols; c0 += 16) {
+                    const float v = __bfloat162float(p.v_cache[(row * p.Hkv + c.g) * D + key % D]);
+                    for (int c0 = col0; c0 < min(cols, col0 + WIDE); c0 += 16) {
                         uint32_t x[16];
                         tmem_ld16(tmem_O + c0 + lane_sel, x);
                         tmem_wait_ld();
@@ -417,137 +446,129 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 s_at[which * COLS + tid] = tid < c.u.cols ? c.u.at0 + t : -1;
                 s_row[which * COLS + tid] = tid < c.u.cols ? (c.u.s * p.n_new + c.u.tok0 + t) * p.Hq + c.g * G + (tid - t * G) : -1;
             }
-            named_bar_sync(1, 128);
+            named_bar_sync(1, WORKERS);
             // column, 16-byte chunk of its row: box, then chunk ^ (column % 8) of the 128-byte row; columns past the last are zero
-            constexpr int NQ = COLS * (D / 8) / 128;         // chunks a thread, all on their way before the first is stored
+            constexpr int NQ = COLS * (D / 8) / WORKERS;     // chunks a thread, all on their way before the first is stored
             uint4 v[NQ];
 #pragma unroll
             for (int k = 0; k < NQ; ++k) {
-                const int i = tid + k * 128, row = s_row[which * COLS + i / (D / 8)];
+                const int i = tid + k * WORKERS, row = s_row[which * COLS + i / (D / 8)];
                 v[k] = row >= 0 ? *reinterpret_cast<const uint4*>(p.q + (size_t)row * D + (i % (D / 8)) * 8) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
             for (int k = 0; k < NQ; ++k) {
-                const int i = tid + k * 128, col = i / (D / 8), c16 = i % (D / 8);
+                const int i = tid + k * WORKERS, col = i / (D / 8), c16 = i % (D / 8);
                 *reinterpret_cast<uint4*>(sgen + SM::OFF_Q + (c16 >> 3) * QBOX + col * 128 + (((c16 & 7) ^ (col & 7)) << 4)) = v[k];
             }
             fence_proxy_async();
             mbar_arrive(bar_q);
         };
         load_q(0);
-        fetch_pids(c);
         bool to_patch = false;
         int before_k0 = 0, left = my_tiles, which = 0;
         bool first = true;                                      // of the head's tiles in this CTA
         for (int it = 0; it < my_tiles; ++it) {
             const WindowUnit& u = c.u;
-            const int k0 = u.key_of(c.i), j = k0 + tid, cols = u.cols, at0 = u.at0, end = u.end;
+            const int k0 = u.key_of(c.i), j = k0 + key, cols = u.cols, at0 = u.at0, end = u.end;
             at_of = s_at + which * COLS;
             const bool last = --left == 0 || c.i + 1 == u.tiles;
-            mbar_wait(bar_s, it & 1, abort_flag, status);       // S^T ready; V, P^T free; O^T up to date
+            mbar_wait(bar_s + (it & 1) * 8, (it >> 1) & 1, abort_flag, status);          // S^T ready
             tc_fence_after();
-            if (to_patch) {                                     // the same decision in every thread
-                patch(before_k0);
-                named_bar_sync(1, 128);                         // P^T is written again below
-            }
-            if (!PAGES) {
-                load_v_rows(k0);
-                if (!last) {
-                    ++c.i;
-                    fetch_pids(c);
-                    --c.i;
-                }
-            }
             // some query does not see some key of the tile
             const bool masked = k0 + 127 > at0 || !(k0 + 127 < p.sinks || end - 1 - k0 < p.window);
-            float sc[COLS];
+            // scores of CH columns from c0, read where they are needed: there is no room to hold them all.  Columns come in blocks without a
+            // branch inside, so that a block's loads and exponentials overlap.
+            auto scores = [&](int c0, float (&sc)[CH], float (&ref)[CH]) {
+                uint32_t r[16];
+                tmem_ld16(tmem_S + (it & 1) * COLS + c0 + lane_sel, r);
 #pragma unroll
-            for (int c0 = 0; c0 < COLS; c0 += 16)
-                if (c0 < cols) {
-                    uint32_t r[16];
-                    tmem_ld16(tmem_S + c0 + lane_sel, r);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) sc[c0 + x] = __uint_as_float(r[x]) * p.scale_log2;
+                for (int x = 0; x < CH; x += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(s_ref + c0 + x);
+                    ref[x] = y.x;
+                    ref[x + 1] = y.y;
+                    ref[x + 2] = y.z;
+                    ref[x + 3] = y.w;
                 }
-            // in blocks of 8 columns, without a branch inside, so that a block's loads and exponentials overlap
-            if (masked) {
+                tmem_wait_ld();
 #pragma unroll
-                for (int c0 = 0; c0 < COLS; c0 += 8)
-                    if (c0 < cols) {
+                for (int x = 0; x < CH; ++x) sc[x] = __uint_as_float(r[x]) * p.scale_log2;
+                if (masked) {
 #pragma unroll
-                        for (int x = c0; x < c0 + 8; ++x) sc[x] = sees(j, at_of[x]) ? sc[x] : -INFINITY;
-                    }
-            }
+                    for (int x = 0; x < CH; ++x) sc[x] = sees(j, at_of[c0 + x]) ? sc[x] : -INFINITY;
+                }
+            };
             bool above = false;
 #pragma unroll
-            for (int c0 = 0; c0 < COLS; c0 += 8)
-                if (c0 < cols) {
-                    const float4 a = *reinterpret_cast<const float4*>(s_ref + c0), b = *reinterpret_cast<const float4*>(s_ref + c0 + 4);
-                    const float ref[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            for (int c0 = 0; c0 < WIDE; c0 += CH)
+                if (col0 + c0 < cols) {
+                    float sc[CH], ref[CH];
+                    scores(col0 + c0, sc, ref);
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) above |= sc[c0 + x] - ref[x] > 8.0f;
+                    for (int x = 0; x < CH; ++x) above |= sc[x] - ref[x] > 8.0f;
                 }
-            if (group_any(1, 128, above)) {
+            const bool grow = group_any(1, WORKERS, above);
+            if (it > 0) mbar_wait(bar_done, (it - 1) & 1, abort_flag, status);           // P^T is free, O^T up to date
+            if (it > 0) tc_fence_after();
+            if (to_patch) {                                     // the same decision in every thread
+                patch(before_k0);
+                named_bar_sync(1, WORKERS);                     // P^T is written again below
+            }
+            if (grow) {
                 // the columns' maxima over the tile; the references that are too low move there
 #pragma unroll
-                for (int c0 = 0; c0 < COLS; c0 += 8)
-                    if (c0 < cols) {
+                for (int c0 = 0; c0 < WIDE; c0 += CH)
+                    if (col0 + c0 < cols) {
+                        float sc[CH], ref[CH];
+                        scores(col0 + c0, sc, ref);
 #pragma unroll
-                        for (int x = c0; x < c0 + 8; ++x) {
+                        for (int x = 0; x < CH; ++x) {
                             const int m = __reduce_max_sync(0xffffffffu, window_order(sc[x]));
-                            if (lane == 0) s_wmax[warp * COLS + x] = window_unorder(m);
+                            if (lane == 0) s_wmax[(warp & 3) * COLS + col0 + c0 + x] = window_unorder(m);
                         }
                     }
-                named_bar_sync(1, 128);
-                if (tid < cols) {
+                named_bar_sync(1, WORKERS);
+                if (tid < COLS) {
                     const float top = fmaxf(fmaxf(s_wmax[tid], s_wmax[COLS + tid]), fmaxf(s_wmax[2 * COLS + tid], s_wmax[3 * COLS + tid]));
-                    const float ref = s_ref[tid], to = top - ref > 8.0f ? top : ref;
+                    const float ref = s_ref[tid], to = tid < cols && top - ref > 8.0f ? top : ref;
                     s_alpha[tid] = fast_exp2(ref - to);
                     s_ref[tid] = to;
                 }
-                named_bar_sync(1, 128);
+                named_bar_sync(1, WORKERS);
 #pragma unroll
-                for (int c0 = 0; c0 < COLS; c0 += 8)
-                    if (c0 < cols) {
-#pragma unroll
-                        for (int x = c0; x < c0 + 8; ++x) l_part[x] *= x < cols ? s_alpha[x] : 1.f;
-                    }
-                if (!first) {                     // O^T row d = tid
-                    for (int c0 = 0; c0 < cols; c0 += 16) {
+                for (int x = 0; x < WIDE; ++x) l_part[x] *= s_alpha[col0 + x];
+                if (!first) {                     // O^T row d = key
+                    for (int c0 = col0; c0 < min(cols, col0 + WIDE); c0 += 16) {
                         uint32_t o[16];
                         tmem_ld16(tmem_O + c0 + lane_sel, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * (c0 + x < cols ? s_alpha[c0 + x] : 0.f));
+                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * s_alpha[c0 + x]);
                         tmem_st16(tmem_O + c0 + lane_sel, o);
                         tmem_wait_st();
                     }
                 }
             }
-            // weights of key tid -> P^T[c][tid] (bf16), row c of box tid / 64
-            uint8_t* prow = sgen + SM::OFF_P + (tid >> 6) * QBOX + ((tid & 7) << 1);
-            const int chunk = (tid & 63) >> 3;
+            // weights of this key -> P^T[column][key] (bf16), row `column` of box key / 64
+            uint8_t* prow = sgen + SM::OFF_P + (key >> 6) * QBOX + ((key & 7) << 1);
+            const int chunk = (key & 63) >> 3;
 #pragma unroll
-            for (int c0 = 0; c0 < COLS; c0 += 8)
-                if (c0 < cols) {
-                    const float4 a = *reinterpret_cast<const float4*>(s_ref + c0), b = *reinterpret_cast<const float4*>(s_ref + c0 + 4);
-                    const float ref[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            for (int c0 = 0; c0 < WIDE; c0 += CH)
+                if (col0 + c0 < cols) {
+                    float sc[CH], ref[CH];
+                    scores(col0 + c0, sc, ref);
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        const float w = fast_exp2(sc[c0 + x] - ref[x]);
+                    for (int x = 0; x < CH; ++x) {
+                        const float w = fast_exp2(sc[x] - ref[x]);
                         l_part[c0 + x] += w;
-                        *reinterpret_cast<__nv_bfloat16*>(prow + (c0 + x) * 128 + ((chunk ^ x) << 4)) = __float2bfloat16(w);
+                        *reinterpret_cast<__nv_bfloat16*>(prow + (col0 + c0 + x) * 128 + ((chunk ^ (x & 7)) << 4)) = __float2bfloat16(w);
                     }
                 }
-            if (!PAGES) asm volatile("cp.async.wait_group 0;" ::: "memory");
             to_patch = false;
             if (masked) {                         // the same decision in every thread
-                if (PAGES) mbar_wait(bar_vfull, it & 1, abort_flag, status);
-                else named_bar_sync(1, 128);      // other threads fetched this thread's row
-                bool clear = !u.seen_by_some(j), bad = false;
-                uint4* vrow = reinterpret_cast<uint4*>(sgen + SM::OFF_V + tid * 128);
-                if (!clear && !(sees(j, at0) && sees(j, end - 1))) {
+                mbar_wait(bar_vfull, it & 1, abort_flag, status);
+                bool clear = tid < 128 && !u.seen_by_some(j), bad = false;
+                uint4* vrow = reinterpret_cast<uint4*>(sgen + SM::OFF_V + key * 128);
+                if (tid < 128 && !clear && !(sees(j, at0) && sees(j, end - 1))) {
                     // some see it and others do not (or may not): it has to be finite
 #pragma unroll
                     for (int b = 0; b < NBOX; ++b)
@@ -560,14 +581,14 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         }
                 }
                 const uint32_t bads = __ballot_sync(0xffffffffu, bad);
-                if (lane == 0) s_bad[warp] = bads;
+                if (lane == 0 && warp < 4) s_bad[warp] = bads;
                 if (clear || bad) {
 #pragma unroll
                     for (int b = 0; b < NBOX; ++b)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) vrow[b * (BOX / 16) + i] = make_uint4(0, 0, 0, 0);
                 }
-                to_patch = group_any(1, 128, bad);
+                to_patch = group_any(1, WORKERS, bad);
             }
             fence_proxy_async();      // P^T and the V rows written by this thread visible to the tensor core's reads of shared memory
             tc_fence_before();
@@ -586,7 +607,6 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 c.next_unit(p);
                 which ^= 1;
                 load_q(which);
-                fetch_pids(c);
             }
             mbar_wait(bar_done, it & 1, abort_flag, status);
             tc_fence_after();
@@ -599,8 +619,8 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             }
             // sums of 8 columns over the warp's lanes: the lanes halve the columns that they hold three times, then add twice
 #pragma unroll
-            for (int c0 = 0; c0 < COLS; c0 += 8)
-                if (c0 < cols) {
+            for (int c0 = 0; c0 < WIDE; c0 += 8)
+                if (col0 + c0 < cols) {
                     float v[8];
 #pragma unroll
                     for (int x = 0; x < 8; ++x) v[x] = l_part[c0 + x];
@@ -615,21 +635,21 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     }
                     v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
                     v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
-                    if ((lane & 3) == 0) s_wmax[warp * COLS + c0 + (lane >> 2)] = v[0];
+                    if ((lane & 3) == 0) s_wmax[(warp & 3) * COLS + col0 + c0 + (lane >> 2)] = v[0];
                 }
-            for (int c0 = 0; c0 < cols; c0 += 16) {
+            for (int c0 = col0; c0 < min(cols, col0 + WIDE); c0 += 16) {
                 uint32_t o[16];
                 tmem_ld16(tmem_O + c0 + lane_sel, o);
                 tmem_wait_ld();
-                if (tid < D) {
+                if (key < D) {
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
                         const int row = s_row[result + c0 + x];
-                        if (row >= 0) p.part_o[((size_t)row * p.nsplit + part) * D + tid] = __uint_as_float(o[x]);
+                        if (row >= 0) p.part_o[((size_t)row * p.nsplit + part) * D + key] = __uint_as_float(o[x]);
                     }
                 }
             }
-            named_bar_sync(1, 128);
+            named_bar_sync(1, WORKERS);
             if (tid < cols) {
                 const float ref = s_ref[tid];
                 float* ml = p.part_ml + ((size_t)s_row[result + tid] * p.nsplit + part) * 2;
@@ -639,16 +659,16 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             if (left > 0) {
                 if (tid < COLS) s_ref[tid] = tid < c.u.cols ? WIN_UNSET : 0.f;
 #pragma unroll
-                for (int x = 0; x < COLS; ++x) l_part[x] = 0.f;
-                named_bar_sync(1, 128);                         // the references are read by all
+                for (int x = 0; x < WIDE; ++x) l_part[x] = 0.f;
+                named_bar_sync(1, WORKERS);                         // the references are read by all
             }
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 4) {
+    if (warp == CONTROL) {
         __syncwarp();
-        tmem_dealloc(tmem_S, 2 * COLS);
+        tmem_dealloc(tmem_S, 4 * COLS);
     }
 }
 
@@ -689,7 +709,7 @@ int launch_window(const CUtensorMap& tk, const CUtensorMap& tv, const WindowPara
     constexpr int bytes = WinSmem<D, COLS>::DYN_BYTES, resident = WinSmem<D, COLS>::CTAS;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return cuda_refused();
     const long long ctas = most_tiles < 148 * resident ? most_tiles : 148 * resident;        // one wave
-    return launch_after(kern, dim3((unsigned)(ctas < 1 ? 1 : ctas)), WIN_THREADS, bytes, st, tk, tv, p);
+    return launch_after(kern, dim3((unsigned)(ctas < 1 ? 1 : ctas)), WinSmem<D, COLS>::THREADS, bytes, st, tk, tv, p);
 }
 template <int D>
 int launch_window_cols(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, const MergeParams& m, long long most_tiles, bool pages,
