@@ -414,6 +414,20 @@ __device__ __forceinline__ int float_order(float x) {
 }
 __device__ __forceinline__ float float_unorder(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 
+// Rows of the cache are read once.  Where scores are written they leave the L2 cache first, so that the scores, which are read again
+// behind the last of them, stay there.
+__device__ __forceinline__ void tma_load_3d_first_out(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ uint64_t first_out_policy() {
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
+}
+
 template <int G, int LOAD, bool SCORES>
 __global__ void __launch_bounds__(DTC_THREADS, 3)
 decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, DecodeParams p) {
@@ -510,6 +524,11 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
                 }
             }
         };
+        const uint64_t policy = SCORES ? first_out_policy() : 0;
+        auto load_box = [&](uint32_t dst, const CUtensorMap* map, int c0, int row, uint32_t bar) {
+            if (SCORES) tma_load_3d_first_out(dst, map, c0, g, row, bar, policy);
+            else tma_load_3d(dst, map, c0, g, row, bar);
+        };
         auto load_k = [&](int tt, const Ids& id) {          // K buffer must be free
             if (PAGES) {
                 const int npages = min(ppt, (n - tt * 128 + ps - 1) / ps);
@@ -518,8 +537,8 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
                 __syncwarp();
                 if (lane < npages) {
                     const uint32_t off = (uint32_t)(lane * ps) * 128u;
-                    tma_load_3d(sK + off, &tm_k, 0, g, row, bar_kfull);
-                    tma_load_3d(sK + BOX + off, &tm_k, 64, g, row, bar_kfull);
+                    load_box(sK + off, &tm_k, 0, row, bar_kfull);
+                    load_box(sK + BOX + off, &tm_k, 64, row, bar_kfull);
                 }
             } else {
                 const int nvalid = min(128, n - tt * 128);
@@ -547,8 +566,8 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             __syncwarp();
             if (lane < npages) {
                 const uint32_t off = (uint32_t)(lane * ps) * 128u;
-                tma_load_3d(sV + off, &tm_v, 0, g, row, bar_vfull);
-                tma_load_3d(sV + BOX + off, &tm_v, 64, g, row, bar_vfull);
+                load_box(sV + off, &tm_v, 0, row, bar_vfull);
+                load_box(sV + BOX + off, &tm_v, 64, row, bar_vfull);
             }
         };
         Ids cur, nxt;

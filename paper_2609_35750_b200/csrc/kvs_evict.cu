@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) evict_plan_kernel(EvictParams p)
     pdl_wait();
     const int top = hdr->top;
     int sum = 0, total;
-    for (int s = threadIdx.x; s < p.S; s += PLAN_THREADS) {
+    for (int s = threadIdx.x; s < p.S; s += blockDim.x) {
         const int n = p.n_tokens[s];
         if (n >= 0 && pages_of(n, p.page_size) <= p.max_pages) sum += pages_to_leave(p, n);
         else set_status(&hdr->status, KVS_ERR_INVALID_ARG);          // a length that the table cannot hold: this sequence stays as it is
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) evict_plan_kernel(EvictParams p)
         if (fits) hdr->top = top + total;
         else set_status(&hdr->status, KVS_ERR_INVALID_ARG);
     }
-    for (int s = threadIdx.x; s < p.S; s += PLAN_THREADS) {
+    for (int s = threadIdx.x; s < p.S; s += blockDim.x) {
         const int n = p.n_tokens[s];
         const int take = fits && n >= 0 && pages_of(n, p.page_size) <= p.max_pages ? pages_to_leave(p, n) : 0;
         p.n_evicted[s] = take;
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
     auto needs = [&](int n) { return pages_of(n + p.n_new, p.page_size) - pages_of(n, p.page_size); };
     const int top = hdr->top;
     int sum = 0, total;
-    for (int s = tid; s < p.S; s += PLAN_THREADS) {
+    for (int s = tid; s < p.S; s += blockDim.x) {
         if (!joins(s)) continue;
         const int n = p.n_tokens[s];
         const long long room = (long long)p.max_pages * p.page_size;
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
     }
     if (no != KVS_OK) return;                            // the same in the whole CTA
     int base = 0;
-    for (int s0 = 0; s0 < p.S; s0 += PLAN_THREADS) {
+    for (int s0 = 0; s0 < p.S; s0 += blockDim.x) {
         const int s = s0 + tid;
         const bool in = joins(s);
         const int n = in ? p.n_tokens[s] : 0, need = in ? needs(n) : 0;
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
         base += here;
         if (in) p.n_tokens[s] = n + p.n_new;
         __syncthreads();
-        for (int i = tid >> 5; i < min(PLAN_THREADS, p.S - s0); i += PLAN_THREADS / 32) {        // a warp for a sequence
+        for (int i = tid >> 5; i < min((int)blockDim.x, p.S - s0); i += blockDim.x / 32) {        // a warp for a sequence
             if (s_n[i] < 0) continue;
             const int slot = pages_of(s_n[i], p.page_size), pages = needs(s_n[i]);
             for (int j = tid & 31; j < pages; j += 32)
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) truncate_kernel(int n_drafted, c
     };
     const int top = hdr->top;
     int sum = 0, total;
-    for (int s = tid; s < S; s += PLAN_THREADS) {
+    for (int s = tid; s < S; s += blockDim.x) {
         const int n = n_tokens[s], gone = leaves(s, n, true);
         sum += gone > 0 ? pages_of(n, page_size) - pages_of(n - gone, page_size) : 0;
     }
@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) truncate_kernel(int n_drafted, c
     }
     if (!fits) return;                                   // the same in the whole CTA
     int base = 0;
-    for (int s0 = 0; s0 < S; s0 += PLAN_THREADS) {
+    for (int s0 = 0; s0 < S; s0 += blockDim.x) {
         const int s = s0 + tid, n = s < S ? n_tokens[s] : 0, gone = s < S ? leaves(s, n, false) : 0;
         const int pages = gone > 0 ? pages_of(n, page_size) - pages_of(n - gone, page_size) : 0;
         int here;
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) truncate_kernel(int n_drafted, c
         base += here;
         if (gone > 0) n_tokens[s] = n - gone;
         __syncthreads();
-        for (int i = tid >> 5; i < min(PLAN_THREADS, S - s0); i += PLAN_THREADS / 32) {          // a warp for a sequence
+        for (int i = tid >> 5; i < min((int)blockDim.x, S - s0); i += blockDim.x / 32) {          // a warp for a sequence
             if (s_from[i] >= s_to[i]) continue;
             const int slot = pages_of(s_from[i], page_size), end = pages_of(s_to[i], page_size);
             for (int j = tid & 31; j < end - slot; j += 32)
@@ -405,6 +405,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) truncate_kernel(int n_drafted, c
 
 using namespace kvs;
 
+// A thread for a sequence, and a warp for its pages: few sequences need no large CTA
+static int plan_threads(int num_seqs) { return num_seqs <= 32 ? 128 : num_seqs <= 128 ? 256 : PLAN_THREADS; }
 static bool cache_sizes_ok(int num_seqs, int page_size, int max_pages, int num_pages) {
     return num_seqs >= 0 && page_size > 0 && max_pages > 0 && num_pages > 0;
 }
@@ -432,7 +434,7 @@ extern "C" int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recen
                            n_evicted};
     cudaStream_t st = (cudaStream_t)stream;
     if (smem > 40 * 1024 && cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return cuda_refused();
-    const int rc = launch_after(evict_plan_kernel, 1, PLAN_THREADS, 0, st, p);
+    const int rc = launch_after(evict_plan_kernel, 1, plan_threads(num_seqs), 0, st, p);
     if (rc != KVS_OK) return rc;
     return launch_clusters_after(evict_kernel, dim3((unsigned)(num_seqs * C)), C, EV_THREADS, smem, st, p, cap);
 }
@@ -449,7 +451,7 @@ extern "C" int kvs_cache_append_tokens(const void* k_new, const void* v_new, con
     const JoinParams p = {(const __nv_bfloat16*)k_new, (const __nv_bfloat16*)v_new, active, num_seqs, n_new, Hkv * head_dim, page_size, max_pages, num_pages,
                           block_table, n_tokens, free_list, (__nv_bfloat16*)k_cache, (__nv_bfloat16*)v_cache};
     cudaStream_t st = (cudaStream_t)stream;
-    const int rc = launch_after(join_plan_kernel, 1, PLAN_THREADS, 0, st, p);
+    const int rc = launch_after(join_plan_kernel, 1, plan_threads(num_seqs), 0, st, p);
     if (rc != KVS_OK) return rc;
     const bool wide = (p.row % 8) == 0 && (rows & 15) == 0;
     const long long items = (long long)num_seqs * n_new * (wide ? p.row / 8 : p.row);
@@ -465,6 +467,6 @@ extern "C" int kvs_cache_truncate(int n_drafted, const int32_t* n_accepted, int 
     if (!n_accepted || !block_table || !n_tokens || !free_list) return KVS_ERR_INVALID_ARG;
     if ((((uintptr_t)n_accepted | (uintptr_t)block_table | (uintptr_t)n_tokens | (uintptr_t)free_list | (uintptr_t)token_weight) & 3) != 0)
         return KVS_ERR_ALIGNMENT;
-    return launch_after(truncate_kernel, 1, PLAN_THREADS, 0, (cudaStream_t)stream, n_drafted, n_accepted, num_seqs, page_size, max_pages, num_pages, block_table,
+    return launch_after(truncate_kernel, 1, plan_threads(num_seqs), 0, (cudaStream_t)stream, n_drafted, n_accepted, num_seqs, page_size, max_pages, num_pages, block_table,
                         n_tokens, free_list, token_weight);
 }

@@ -197,7 +197,7 @@ extern "C" int kvs_verify_drafts(const float* target_probs, const float* draft_p
         return KVS_ERR_ALIGNMENT;
     const int tiles = (vocab + VER_TILE - 1) / VER_TILE;
     int C = 8;
-    while (C > 1 && ((long long)num_seqs * C >= 8 * 148 || tiles < C)) C >>= 1;
+    while (C > 1 && ((long long)num_seqs * C > 4 * 148 || tiles < C)) C >>= 1;
     if (vocab > (1 << 21)) C = 8;                // the tiles' sums fit into shared memory
     VerifyParams p = {target_probs, draft_probs, draft_tokens, u_accept, u_sample, tokens, n_accepted, n_draft, vocab, (tiles + C - 1) / C * VER_TILE};
     const size_t smem = (size_t)(p.part / VER_TILE) * sizeof(double);

@@ -119,11 +119,25 @@ struct WinSmem {
     static constexpr int DYN_BYTES = TOTAL + 1024;                     // slack for the 1024-byte alignment
 };
 
-__device__ __forceinline__ int window_order(float x) {                 // order-preserving map float -> int
-    const int i = __float_as_int(x);
-    return i ^ ((i >> 31) & 0x7fffffff);
+// 8 values of every lane, each joined over the warp: lane l gets value l / 4.  The lanes halve the values that they hold three times, then
+// join twice: 9 shuffles, where value by value takes 40.
+template <typename F>
+__device__ __forceinline__ float warp_of_8(const float* of, int lane, F join) {
+    float v[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] = of[x];
+#pragma unroll
+    for (int half = 4; half > 0; half >>= 1) {
+        const bool upper = lane & (half * 4);
+#pragma unroll
+        for (int x = 0; x < half; ++x) {
+            const float mine = upper ? v[x + half] : v[x], other = upper ? v[x] : v[x + half];
+            v[x] = join(mine, __shfl_xor_sync(0xffffffffu, other, half * 4));
+        }
+    }
+    v[0] = join(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
+    return join(v[0], __shfl_xor_sync(0xffffffffu, v[0], 2));
 }
-__device__ __forceinline__ float window_unorder(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 // Whether any thread of the group says so, the same answer for each
 __device__ __forceinline__ bool group_any(int id, int nthreads, bool mine) {
     uint32_t any;
@@ -160,17 +174,27 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     // ---- this CTA's share ----
     long long share, at, all;
     {
-        long long sum = 0;
-        int most = 0;
+        // every thread's first entry is kept: with no more entries than threads they are gone over once
         WindowUnit u;
-        for (int e = tid; e < E; e += THREADS) {
-            u.load(p, e);
-            sum += u.tiles;
-            most = max(most, u.tiles);
+        u.tiles = 0;
+        if (tid < E) u.load(p, tid);
+        long long rest = 0, first_sum;
+        int most = u.tiles;
+        for (int e = tid + THREADS; e < E; e += THREADS) {
+            WindowUnit more;
+            more.load(p, e);
+            rest += more.tiles;
+            most = max(most, more.tiles);
         }
         most = __reduce_max_sync(0xffffffffu, most);
         if (lane == 0 && most > 0) atomicMax(&s_most, most);
-        block_prefix(sum, s_scan, all);
+        const long long first_before = block_prefix((long long)u.tiles, s_scan, first_sum);
+        all = first_sum;
+        if (E > THREADS) {
+            long long others;
+            block_prefix(rest, s_scan, others);
+            all += others;
+        }
         all *= p.Hkv;
         // not so small that a head is cut into more parts than there is room for: the first may be cut anywhere
         share = max(max((all + gridDim.x - 1) / gridDim.x, ((long long)s_most + p.nsplit - 3) / (p.nsplit - 1)), 1ll);
@@ -181,17 +205,20 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             *reinterpret_cast<long long*>(p.header + WIN_SHARE_WORD) = share;
         }
         if (at >= all && blockIdx.x != 0) return;          // the same in the whole CTA
-        long long run = 0, here;
-        for (int e0 = 0; e0 < E && (blockIdx.x == 0 || run * p.Hkv <= at); e0 += THREADS) {
-            const int e = e0 + tid;
-            u.tiles = 0;
-            if (e < E) u.load(p, e);
-            const long long before = run + block_prefix((long long)u.tiles, s_scan, here);
+        auto look = [&](int e, long long before) {         // is it this CTA's first entry; the first CTA writes all down
             if (e < E && blockIdx.x == 0) p.entries[e] = {before, u.tiles, 0};
             if (u.tiles > 0 && before * p.Hkv <= at && at < (before + u.tiles) * p.Hkv) {
                 s_entry = e;
                 s_before = before;
             }
+        };
+        look(tid, first_before);
+        long long run = first_sum, here;
+        for (int e0 = THREADS; e0 < E && (blockIdx.x == 0 || run * p.Hkv <= at); e0 += THREADS) {
+            u.tiles = 0;
+            if (e0 + tid < E) u.load(p, e0 + tid);
+            const long long before = run + block_prefix((long long)u.tiles, s_scan, here);
+            look(e0 + tid, before);
             run += here;
         }
         __syncthreads();
@@ -521,9 +548,9 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         float sc[CH], ref[CH];
                         scores(col0 + c0, sc, ref);
 #pragma unroll
-                        for (int x = 0; x < CH; ++x) {
-                            const int m = __reduce_max_sync(0xffffffffu, window_order(sc[x]));
-                            if (lane == 0) s_wmax[(warp & 3) * COLS + col0 + c0 + x] = window_unorder(m);
+                        for (int b = 0; b < CH; b += 8) {
+                            const float m = warp_of_8(sc + b, lane, [](float x, float y) { return fmaxf(x, y); });
+                            if ((lane & 3) == 0) s_wmax[(warp & 3) * COLS + col0 + c0 + b + (lane >> 2)] = m;
                         }
                     }
                 named_bar_sync(1, WORKERS);
@@ -617,25 +644,11 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 c = next;
                 to_patch = false;
             }
-            // sums of 8 columns over the warp's lanes: the lanes halve the columns that they hold three times, then add twice
 #pragma unroll
             for (int c0 = 0; c0 < WIDE; c0 += 8)
                 if (col0 + c0 < cols) {
-                    float v[8];
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) v[x] = l_part[c0 + x];
-#pragma unroll
-                    for (int half = 4; half > 0; half >>= 1) {
-                        const bool upper = lane & (half * 4);
-#pragma unroll
-                        for (int x = 0; x < half; ++x) {
-                            const float mine = upper ? v[x + half] : v[x], other = upper ? v[x] : v[x + half];
-                            v[x] = mine + __shfl_xor_sync(0xffffffffu, other, half * 4);
-                        }
-                    }
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
-                    if ((lane & 3) == 0) s_wmax[(warp & 3) * COLS + col0 + c0 + (lane >> 2)] = v[0];
+                    const float sum = warp_of_8(l_part + c0, lane, [](float x, float y) { return x + y; });
+                    if ((lane & 3) == 0) s_wmax[(warp & 3) * COLS + col0 + c0 + (lane >> 2)] = sum;
                 }
             for (int c0 = col0; c0 < min(cols, col0 + WIDE); c0 += 16) {
                 uint32_t o[16];
