@@ -20,7 +20,7 @@ namespace kvs {
 namespace cg = cooperative_groups;
 
 constexpr int VER_THREADS = 256;
-constexpr int VER_TILE = 512;               // tokens a warp adds up at a time: 16 loads of either row in flight a lane
+constexpr int VER_TILE = 256;               // tokens a warp adds up at a time: 8 loads of either row in flight a lane (512: 4 x 32000 6.6 -> 7.7 us; 1024: 128 x 131071 27 -> 42)
 
 struct VerifyParams {
     const float* target;        // [S, n + 1, V]
