@@ -71,6 +71,7 @@ SIGNATURES = {
     "kvs_decode_window_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "kvs_decode_window_num_splits": (_i, [_i, _i, _i, _i, _i, _i, _i]),
     "kvs_decode_attn_window": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _f, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "kvs_decode_weights_num_splits": (_i, [_i, _i, _i]),
     "kvs_decode_weights_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "kvs_decode_attn_weights": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _f, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "kvs_cache_evict_lowest": (_i, [_i, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),

@@ -1095,6 +1095,17 @@ static int launch_decode(const DecodeParams& p, int G, const void* k_cache, cons
 // Scores of a call with weights: rows of whole tiles, so that a tile's scores start on a 512-byte line
 static size_t score_bytes(int num_seqs, int Hq, int max_tokens) { return sizeof(float) * (size_t)num_seqs * Hq * align_up((size_t)max_tokens, 128); }
 
+extern "C" int kvs_decode_weights_num_splits(int num_seqs, int Hkv, int max_tokens) {
+    const int n = kvs_decode_num_splits(num_seqs, Hkv, max_tokens);
+    if (num_seqs <= 0 || Hkv <= 0 || max_tokens <= 0) return n;
+    // where that leaves SMs without work, splits of fewer than four tiles: a tile takes 2 us, and the merge reads up to 64 splits in one go
+    // (two caches of 900 to 2500 tokens with 8 KV heads: 5 splits 14.7 us, 20 FEWSPLITS)
+    const long long tiles = ((long long)max_tokens + 127) / 128, wave = 3 * 148 / ((long long)num_seqs * Hkv);
+    long long more = wave < tiles ? wave : tiles;
+    if (more > 64) more = 64;
+    return more > n ? (int)more : n;
+}
+
 extern "C" size_t kvs_decode_weights_workspace_bytes(int num_seqs, int Hq, int head_dim, int num_splits, int max_tokens) {
     const size_t n = kvs_decode_workspace_bytes(num_seqs, Hq, head_dim, num_splits);
     if (n == 0 || max_tokens <= 0 || max_tokens > 0x7fffff00) return 0;

@@ -1,7 +1,7 @@
 // The paged cache's life with accumulated attention weights and drafted tokens: the pages with the lowest weight leave, several
 // tokens of every sequence join in one call, the last ones leave again.
 //
-// Every call is two kernels at most.  The first is one CTA: it goes over the sequences' lengths, counts the pages that each takes or
+// Every call is two kernels at most, and one where it is small.  The first is one CTA: it goes over the sequences' lengths, counts the pages that each takes or
 // gives back, and hands every sequence its place on the free stack by a running sum, so that the order of the stack does not depend
 // on which CTA comes first (the counts follow from the lengths alone, whichever pages they turn out to be).  A call that cannot be
 // done for lack of pages is not begun.  The second kernel moves the data.
@@ -31,7 +31,7 @@ __device__ __forceinline__ int pages_of(int tokens, int page_size) { return (int
 constexpr int EV_THREADS = 512;
 constexpr int EV_COPIES = 8;                // of the counts, by lane: scores crowd into a few digits
 constexpr int EV_MOST_CTAS = 8;             // of a cluster
-constexpr int EV_MOST_SMEM = 208 * 1024;
+constexpr int EV_MOST_SMEM = 208 * 1024, EV_PLAIN_SMEM = 32 * 1024;      // dynamic, beside 11 KB; without asking for more than 48 KB
 
 struct EvictParams {
     int budget, keep_first, keep_recent, S, page_size, max_pages, num_pages;
@@ -86,6 +86,10 @@ __device__ __forceinline__ uint32_t score_bits(float x) {
     return (b >> 31) ? ~b : b | 0x80000000u;
 }
 
+// TOGETHER: at most EV_MOST_CTAS sequences, each small enough for a CTA.  They are one cluster: every CTA reads all lengths and forms the
+// plan itself, and nothing is written before all have, so that one launch does what takes two otherwise (four caches of 5000 tokens in
+// pages of 16 15.7 -> TOGETHERFIG us).
+template <bool TOGETHER>
 __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int cap) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ int s_hist[2][256];               // digits of this CTA's candidates, for the cluster
@@ -95,25 +99,63 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     __shared__ int s_bin, s_below, s_in_bin;
     __shared__ int2 s_counts;
     cg::cluster_group cluster = cg::this_cluster();
-    const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
+    const int C = TOGETHER ? 1 : (int)cluster.num_blocks(), c = TOGETHER ? 0 : (int)cluster.block_rank();
     const int s = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31;
     const int ps = p.page_size;
+    auto sync = [&]() {                          // of a sequence's CTAs
+        if (TOGETHER) __syncthreads();
+        else cluster.sync();
+    };
     float* s_w = reinterpret_cast<float*>(smem_raw);                              // [cap * ps] weights
     int32_t* s_page = reinterpret_cast<int32_t*>(s_w + (size_t)cap * ps);         // [cap] table entries
     uint16_t* s_src = reinterpret_cast<uint16_t*>(s_page + cap);                  // [cap] pages that stay, in order
     uint32_t* s_key = reinterpret_cast<uint32_t*>(s_src + ((cap + 1) & ~1));      // [cap] scores (pages of one token: formed from s_w)
     pdl_wait();
-    const int take = p.n_evicted[s];
+    int take, n, base;                           // pages that leave, live tokens, this sequence's place behind what those before it give back
+    int32_t* stack;                              // the j-th page goes to stack[-j]
+    CacheHeader* hdr = reinterpret_cast<CacheHeader*>(p.free_buf);
+    if (TOGETHER) {
+        int takes[EV_MOST_CTAS], total = 0, bad = 0;
+        base = take = n = 0;
+        const int top = hdr->top;
+#pragma unroll
+        for (int i = 0; i < EV_MOST_CTAS; ++i) {
+            const int ni = i < p.S ? p.n_tokens[i] : 0;
+            const bool ok = ni >= 0 && pages_of(ni, ps) <= p.max_pages;
+            bad |= !ok;
+            takes[i] = ok ? pages_to_leave(p, ni) : 0;
+            base += i < s ? takes[i] : 0;
+            if (i == s) {
+                n = ni;
+                take = takes[i];
+            }
+            total += takes[i];
+        }
+        const bool fits = top >= 0 && total <= p.num_pages - top;
+        if (!fits) take = 0;
+        cluster.sync();                          // all have read: now it may be written
+        if (tid == 0) {
+            p.n_evicted[s] = take;
+            if (take > 0) p.n_tokens[s] = n - take * ps;
+            if (s == 0 && fits) hdr->top = top + total;
+            if (s == 0 && (bad || !fits)) set_status(&hdr->status, KVS_ERR_INVALID_ARG);
+        }
+        stack = p.free_buf + 4 + (top + total - 1 - base);
+    } else {
+        take = p.n_evicted[s];
+    }
     int32_t* evicted = p.evicted ? p.evicted + (size_t)s * p.max_pages : nullptr;
     if (evicted)
         for (int i = take + c * EV_THREADS + tid; i < p.max_pages; i += C * EV_THREADS) evicted[i] = -1;
-    if (take <= 0) return;                               // the same in the whole cluster
-    // this sequence's place on the stack: behind what the sequences before it give back
-    int mine = 0, base;
-    for (int i = tid; i < s; i += EV_THREADS) mine += p.n_evicted[i];
-    block_prefix(mine, s_warp, base);
-    int32_t* stack = p.free_buf + 4 + (reinterpret_cast<CacheHeader*>(p.free_buf)->top - 1 - base);       // the j-th page goes to stack[-j]
-    const int n = p.n_tokens[s] + take * ps, live = pages_of(n, ps);
+    if (take <= 0) return;                               // the same in the whole cluster (TOGETHER: its CTAs do not meet again)
+    if (!TOGETHER) {
+        int mine = 0;
+        for (int i = tid; i < s; i += EV_THREADS) mine += p.n_evicted[i];
+        block_prefix(mine, s_warp, base);
+        stack = p.free_buf + 4 + (hdr->top - 1 - base);
+        n = p.n_tokens[s] + take * ps;
+    }
+    const int live = pages_of(n, ps);
     int lo, hi;
     candidates(p, n, lo, hi);
     const int per = (live + C - 1) / C, first = min(c * per, live), count = min(first + per, live) - first;
@@ -154,12 +196,12 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
             hist[tid] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
             copies[0] = copies[1] = make_int4(0, 0, 0, 0);
         }
-        cluster.sync();
+        sync();
         int sum = 0;
         if (tid < 256) {
             int part[EV_MOST_CTAS];                      // all on their way before the first is added: a remote read takes most of a microsecond
 #pragma unroll
-            for (int i = 0; i < EV_MOST_CTAS; ++i) part[i] = i < C ? cluster.map_shared_rank(hist, i)[tid] : 0;
+            for (int i = 0; i < EV_MOST_CTAS; ++i) part[i] = TOGETHER ? (i == 0 ? hist[tid] : 0) : i < C ? cluster.map_shared_rank(hist, i)[tid] : 0;
 #pragma unroll
             for (int i = 0; i < EV_MOST_CTAS; ++i) sum += part[i];
         }
@@ -194,11 +236,11 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     const int under_all = (int)(both >> 32), on_all = (int)(both & 0xffffffffu);
     int under_before = (int)(before >> 32), on_before = (int)(before & 0xffffffffu);
     if (tid == 0) s_counts = make_int2(under_all, on_all);
-    cluster.sync();
+    sync();
     int under_first = 0, on_first = 0, on_total = 0, under_total = 0;
     int2 other[EV_MOST_CTAS];
 #pragma unroll
-    for (int i = 0; i < EV_MOST_CTAS; ++i) other[i] = i < C ? *cluster.map_shared_rank(&s_counts, i) : make_int2(0, 0);
+    for (int i = 0; i < EV_MOST_CTAS; ++i) other[i] = TOGETHER ? (i == 0 ? s_counts : make_int2(0, 0)) : i < C ? *cluster.map_shared_rank(&s_counts, i) : make_int2(0, 0);
 #pragma unroll
     for (int i = 0; i < EV_MOST_CTAS; ++i) {
         if (i < c) {
@@ -246,7 +288,7 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     }
     // no weight behind the last page
     for (int i = (live - take) * ps + c * EV_THREADS + tid; i < live * ps; i += C * EV_THREADS) weight[i] = 0.f;
-    cluster.sync();                                      // the others have read this CTA's counts
+    if (!TOGETHER) cluster.sync();                       // the others have read this CTA's counts
 }
 
 // ---- several tokens of every sequence join --------------------------------------------------------------
@@ -314,6 +356,68 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
                 p.block_table[(size_t)(s0 + i) * p.max_pages + slot + j] = stack[top - 1 - (s_at[i] + j)];
         }
         __syncthreads();
+    }
+}
+
+// Few rows: both steps in one launch, by one cluster.  Every CTA forms the plan itself and nothing is written before all have read; a new
+// page's number comes from the stack and not from the table, which the first CTA fills in meanwhile.
+constexpr int JOIN_CTAS = 8, JOIN_THREADS = 512, JOIN_SEQS = 128;
+template <typename T>
+__global__ void __launch_bounds__(JOIN_THREADS) join_together_kernel(JoinParams p) {
+    __shared__ int s_warp[33];
+    __shared__ int s_no;
+    __shared__ int s_n[JOIN_SEQS], s_at[JOIN_SEQS];
+    cg::cluster_group cluster = cg::this_cluster();
+    CacheHeader* hdr = reinterpret_cast<CacheHeader*>(p.free_buf);
+    const int32_t* stack = p.free_buf + 4;
+    const int tid = threadIdx.x, c = (int)cluster.block_rank();
+    constexpr int PER = sizeof(T) / sizeof(__nv_bfloat16);
+    const int words = p.row / PER;
+    if (tid == 0) s_no = KVS_OK;
+    __syncthreads();
+    pdl_wait();
+    const int top = hdr->top;
+    int need = 0, total;
+    if (tid < JOIN_SEQS) {
+        const bool in = tid < p.S && (!p.active || p.active[tid]);
+        const int n = in ? p.n_tokens[tid] : 0;
+        const long long room = (long long)p.max_pages * p.page_size;
+        if (n < 0 || n > room) s_no = KVS_ERR_INVALID_ARG;
+        else if (in && n > room - p.n_new) s_no = KVS_ERR_WORKSPACE;
+        else if (in) need = pages_of(n + p.n_new, p.page_size) - pages_of(n, p.page_size);
+        s_n[tid] = in ? n : -1;
+    }
+    const int at = block_prefix(need, s_warp, total);
+    if (tid < JOIN_SEQS) s_at[tid] = at;
+    int no = s_no;
+    if (no == KVS_OK && (top < 0 || top > p.num_pages)) no = KVS_ERR_INVALID_ARG;
+    if (no == KVS_OK && total > top) no = KVS_ERR_WORKSPACE;
+    cluster.sync();                                      // all have read: now it may be written (and the sums are in place)
+    if (c == 0 && tid == 0) {
+        hdr->refused = no != KVS_OK;
+        if (no == KVS_OK) hdr->top = top - total;
+        else set_status(&hdr->status, no);
+    }
+    if (no != KVS_OK) return;                            // the same in the whole cluster
+    if (c == 0 && tid < p.S && s_n[tid] >= 0) {
+        p.n_tokens[tid] = s_n[tid] + p.n_new;
+        const int slot = pages_of(s_n[tid], p.page_size);
+        for (int j = 0; j < need; ++j) p.block_table[(size_t)tid * p.max_pages + slot + j] = stack[top - 1 - (at + j)];
+    }
+    const int items = p.S * p.n_new * words;
+    for (int i = c * JOIN_THREADS + tid; i < items; i += JOIN_CTAS * JOIN_THREADS) {
+        const int token = i / words, w = i - token * words, s = token / p.n_new;
+        if (s_n[s] < 0) continue;
+        const int pos = s_n[s] + (token - s * p.n_new), slot = pos / p.page_size, fresh = slot - pages_of(s_n[s], p.page_size);
+        const T k = reinterpret_cast<const T*>(p.k_new)[i], v = reinterpret_cast<const T*>(p.v_new)[i];
+        const int page = fresh >= 0 ? stack[top - 1 - (s_at[s] + fresh)] : p.block_table[(size_t)s * p.max_pages + slot];
+        if ((unsigned)page >= (unsigned)p.num_pages) {               // an entry that names no page of this cache is not followed
+            set_status(&hdr->status, KVS_ERR_INVALID_ARG);
+            continue;
+        }
+        const size_t dst = ((size_t)page * p.page_size + (pos - slot * p.page_size)) * words + w;
+        reinterpret_cast<T*>(p.k_cache)[dst] = k;
+        reinterpret_cast<T*>(p.v_cache)[dst] = v;
     }
 }
 
@@ -433,10 +537,14 @@ extern "C" int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recen
     const EvictParams p = {budget, keep_first, keep_recent, num_seqs, page_size, max_pages, num_pages, block_table, n_tokens, free_list, token_weight, evicted,
                            n_evicted};
     cudaStream_t st = (cudaStream_t)stream;
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return cuda_refused();
+    const size_t alone = (size_t)((max_pages + 2) * page_bytes);
+    if (num_seqs <= EV_MOST_CTAS && max_pages <= 2048 && alone <= EV_PLAIN_SMEM)
+        return launch_clusters_after(evict_kernel<true>, dim3((unsigned)num_seqs), num_seqs, EV_THREADS, alone, st, p, max_pages);
+    if (smem > EV_PLAIN_SMEM && cudaFuncSetAttribute(evict_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        return cuda_refused();
     const int rc = launch_after(evict_plan_kernel, 1, plan_threads(num_seqs), 0, st, p);
     if (rc != KVS_OK) return rc;
-    return launch_clusters_after(evict_kernel, dim3((unsigned)(num_seqs * C)), C, EV_THREADS, smem, st, p, cap);
+    return launch_clusters_after(evict_kernel<false>, dim3((unsigned)(num_seqs * C)), C, EV_THREADS, smem, st, p, cap);
 }
 
 extern "C" int kvs_cache_append_tokens(const void* k_new, const void* v_new, const uint8_t* active, int num_seqs, int n_new, int Hkv, int head_dim,
@@ -451,10 +559,14 @@ extern "C" int kvs_cache_append_tokens(const void* k_new, const void* v_new, con
     const JoinParams p = {(const __nv_bfloat16*)k_new, (const __nv_bfloat16*)v_new, active, num_seqs, n_new, Hkv * head_dim, page_size, max_pages, num_pages,
                           block_table, n_tokens, free_list, (__nv_bfloat16*)k_cache, (__nv_bfloat16*)v_cache};
     cudaStream_t st = (cudaStream_t)stream;
-    const int rc = launch_after(join_plan_kernel, 1, plan_threads(num_seqs), 0, st, p);
-    if (rc != KVS_OK) return rc;
     const bool wide = (p.row % 8) == 0 && (rows & 15) == 0;
     const long long items = (long long)num_seqs * n_new * (wide ? p.row / 8 : p.row);
+    // the cluster has 4096 threads: up to four words each they are faster than a second launch
+    if (num_seqs <= JOIN_SEQS && items <= 4 * JOIN_CTAS * JOIN_THREADS)
+        return wide ? launch_clusters_after(join_together_kernel<uint4>, JOIN_CTAS, JOIN_CTAS, JOIN_THREADS, 0, st, p)
+                    : launch_clusters_after(join_together_kernel<uint16_t>, JOIN_CTAS, JOIN_CTAS, JOIN_THREADS, 0, st, p);
+    const int rc = launch_after(join_plan_kernel, 1, plan_threads(num_seqs), 0, st, p);
+    if (rc != KVS_OK) return rc;
     const unsigned grid = (unsigned)((items + 255) / 256 < 148 * 8 ? (items + 255) / 256 : 148 * 8);
     return wide ? launch_after(join_kernel<uint4>, grid, 256, 0, st, p) : launch_after(join_kernel<uint16_t>, grid, 256, 0, st, p);
 }

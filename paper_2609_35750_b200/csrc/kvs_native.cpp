@@ -22,7 +22,7 @@ namespace {
     X(kvs_mask_meta_bytes) X(kvs_mask_meta) X(kvs_mask_meta_keys) X(kvs_mask_meta_evicted) X(kvs_attn_fwd) X(kvs_attn_fwd_packed) \
     X(kvs_attn_fwd_dual) X(kvs_attn_bwd) X(kvs_attn_bwd_packed) X(kvs_attn_bwd_workspace_bytes) X(kvs_permute_rows) X(kvs_rope_qk) \
     X(kvs_cache_append) X(kvs_cache_append_tokens) X(kvs_cache_truncate) X(kvs_cache_evict_lowest) X(kvs_verify_drafts) X(kvs_decode_attn_weights) \
-    X(kvs_decode_weights_workspace_bytes) X(kvs_decode_attn_window) X(kvs_decode_window_num_splits) X(kvs_decode_window_workspace_bytes) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
+    X(kvs_decode_weights_workspace_bytes) X(kvs_decode_weights_num_splits) X(kvs_decode_attn_window) X(kvs_decode_window_num_splits) X(kvs_decode_window_workspace_bytes) X(kvs_decode_num_splits) X(kvs_decode_workspace_bytes) X(kvs_decode_attn)
 #define KVS_POINTER(name) decltype(&::name) name = nullptr;
 struct Library {
     KVS_FUNCTIONS(KVS_POINTER)
@@ -472,7 +472,7 @@ PyObject* decode_weights(PyObject* const* a) {
     const float scale = real(a[6]);
     const int S = (int)c.S, H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[11]), most = given_most ? given_most : (int)(c.P * c.page);
     int splits = whole(a[7]);
-    if (splits <= 0) splits = lib.kvs_decode_num_splits(S, (int)c.Hkv, most);
+    if (splits <= 0) splits = lib.kvs_decode_weights_num_splits(S, (int)c.Hkv, most);
     const at::Tensor ws = given(a[10]) ? tensor(a[10], "workspace") : bytes(lib.kvs_decode_weights_workspace_bytes(S, H, d, splits, most), q);
     const at::Tensor out = out_of(a[8], "out", q), lse = out_of(a[9], "lse", {c.S, Hq}, q, F32);
     void *po = checked(out, "out", BF16, {c.S, Hq, c.d}, q), *pws = checked(ws, "workspace", U8, {-1}, q);

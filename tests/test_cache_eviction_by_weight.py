@@ -121,6 +121,22 @@ def test_lowest_pages_leave(page, max_pages, budget, first, recent):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[0], [1], [300], [999, 0, 17], [15, 16, 17, 33, 128, 300, 1000, 2], [15, 16, 17, 33, 128, 300, 1000, 2, 400]])
+@pytest.mark.parametrize("page,max_pages", [(1, 1003), (16, 70), (5, 400), (1, 2048), (1, 2049), (64, 150)])
+def test_few_sequences(lens, page, max_pages):
+    """Up to eight small sequences are planned and cut by one launch, more or larger ones by two."""
+    c = make(np.random.default_rng([len(lens), page]), lens, page, max_pages)
+    c["weight"][:, 5:9] = 3.0
+    for s, n in enumerate(lens):
+        c["weight"][s, n:] = 0.0
+    g = on_gpu(c)
+    evicted, count = B.kvs_cache_evict_lowest(20, 3, 5, page, g["table"], g["n"], g["free"], g["weight"])
+    want, number = O.evict_lowest(c, 20, 3, 5, page)
+    assert np.array_equal(evicted.cpu().numpy(), want) and np.array_equal(count.cpu().numpy(), number)
+    same(c, g)
+
+
+@pytest.mark.gpu
 def test_more_sequences_than_the_plan_has_threads_and_equal_scores():
     rng = np.random.default_rng(5)
     lens = rng.integers(0, 40, size=2500).tolist()
@@ -149,22 +165,41 @@ def test_largest_cache_of_one_token_pages():
 
 
 @pytest.mark.gpu
-def test_states_that_make_no_sense_are_left_alone():
+@pytest.mark.parametrize("more", [0, 9])                         # by one launch and by two
+def test_states_that_make_no_sense_are_left_alone(more):
     rng = np.random.default_rng(7)
-    c = make(rng, [20, 30], 2, 16)
-    for name, spoil in (("n", lambda x: x.__setitem__(0, 33)), ("n", lambda x: x.__setitem__(0, -5))):
+    c = make(rng, [20, 30] + [4] * more, 2, 16)
+    for value in (33, -5):
         bad = copy.deepcopy(c)
-        spoil(bad[name])
+        bad["n"][0] = value
         g = on_gpu(bad)
         evicted, count = B.kvs_cache_evict_lowest(10, 0, 0, 2, g["table"], g["n"], g["free"], g["weight"])
-        assert int(g["free"][1]) == B.KVS_ERR_INVALID_ARG and count.tolist() == [0, 10] and not (evicted[0] != -1).any()
-        assert g["n"].tolist() == [int(bad["n"][0]), 10] and g["table"][0].cpu().numpy().tolist() == bad["table"][0].tolist()
+        assert int(g["free"][1]) == B.KVS_ERR_INVALID_ARG and count.tolist() == [0, 10] + [0] * more and not (evicted[0] != -1).any()
+        assert g["n"].tolist() == [value, 10] + [4] * more and g["table"][0].cpu().numpy().tolist() == bad["table"][0].tolist()
     bad = copy.deepcopy(c)
-    bad["free"][0] = 27                                          # more pages would come back than the cache has (28)
+    bad["free"][0] = len(c["free"]) - 4 - 1                      # more pages would come back than the cache has
     g = on_gpu(bad)
     _, count = B.kvs_cache_evict_lowest(10, 0, 0, 2, g["table"], g["n"], g["free"], g["weight"])
-    assert int(g["free"][1]) == B.KVS_ERR_INVALID_ARG and not count.any() and int(g["free"][0]) == 27
-    assert g["n"].tolist() == [20, 30] and np.array_equal(g["table"].cpu().numpy(), bad["table"])
+    assert int(g["free"][1]) == B.KVS_ERR_INVALID_ARG and not count.any() and int(g["free"][0]) == bad["free"][0]
+    assert g["n"].tolist() == bad["n"].tolist() and np.array_equal(g["table"].cpu().numpy(), bad["table"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("S,new,Hkv,d", [(128, 3, 1, 64), (129, 3, 1, 64), (300, 1, 2, 128), (2, 300, 4, 128), (1500, 2, 1, 64)])
+def test_many_sequences_and_many_tokens_join(S, new, Hkv, d):
+    rng = np.random.default_rng([S, new])
+    page, lens = 4, rng.integers(0, 30, size=S).tolist()
+    c = make(rng, lens, page, (30 + new) // page + 1, spare=S * (new // page + 2))
+    g = on_gpu(c)
+    kc = torch.zeros((len(c["free"]) - 4, page, Hkv, d), device="cuda", dtype=torch.bfloat16)
+    kn = torch.randn((S, new, Hkv, d), device="cuda").bfloat16()
+    vc, want = kc.clone(), kc.clone()
+    B.kvs_cache_append_tokens(kn, -kn, g["table"], g["n"], g["free"], kc, vc)
+    places = O.append_tokens(c, new, page)
+    at = torch.tensor([places[s][t] for s in range(S) for t in range(new)], device="cuda")
+    want[at[:, 0], at[:, 1]] = kn.view(S * new, Hkv, d)
+    same(c, g)
+    assert torch.equal(kc, want) and torch.equal(vc, -want)
 
 
 @pytest.mark.gpu
@@ -204,11 +239,12 @@ def test_tokens_join_and_leave(page, Hkv, d, new):
 
 
 @pytest.mark.gpu
-def test_tokens_join_all_or_none():
+@pytest.mark.parametrize("d", [64, 1 << 15])                     # by one launch and by two
+def test_tokens_join_all_or_none(d):
     rng = np.random.default_rng(8)
     c = make(rng, [3, 8], 4, 4, spare=4)                        # the call needs 4 pages
-    kn = torch.ones((2, 6, 1, 64), device="cuda").bfloat16()
-    kc = torch.zeros((len(c["free"]) - 4, 4, 1, 64), device="cuda").bfloat16()
+    kn = torch.ones((2, 6, 1, d), device="cuda").bfloat16()
+    kc = torch.zeros((len(c["free"]) - 4, 4, 1, d), device="cuda").bfloat16()
     for spoil, code in ((lambda x: None, B.KVS_OK), (lambda x: x["free"].__setitem__(0, 3), B.KVS_ERR_WORKSPACE),
                         (lambda x: x["n"].__setitem__(1, 11), B.KVS_ERR_WORKSPACE), (lambda x: x["n"].__setitem__(0, -1), B.KVS_ERR_INVALID_ARG),
                         (lambda x: x["n"].__setitem__(0, 17), B.KVS_ERR_INVALID_ARG), (lambda x: x["free"].__setitem__(0, 99), B.KVS_ERR_INVALID_ARG)):
