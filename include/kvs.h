@@ -443,8 +443,8 @@ int kvs_decode_attn_weights(const void* q, const void* k_cache, const void* v_ca
  * evicted: int32 [num_seqs, max_pages], the table slots (before the call) that left, ascending, then -1; may be NULL.  What left is
  * what the trainer's evict_at needs: the caller knows which tokens the slots held.  n_evicted: int32 [num_seqs], pages.
  * n_tokens of a sequence that its table cannot hold: KVS_ERR_INVALID_ARG in the cache status word, that sequence stays as it is.
- * A sequence's weights, table and scores have to fit into the shared memory of a cluster: about 160000 tokens with pages of one token,
- * 380000 with pages of 16; larger max_pages * page_size return KVS_ERR_UNSUPPORTED.
+ * A sequence's weights, table and scores have to fit into the shared memory of a cluster: about 150000 tokens with pages of one or two
+ * tokens, 340000 with pages of 16; larger max_pages * page_size return KVS_ERR_UNSUPPORTED.
  * kvs_cache_evict does not know of token_weight: a cache with weights is not evicted by ranges.
  */
 int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recent,

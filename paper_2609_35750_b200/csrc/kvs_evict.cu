@@ -15,7 +15,8 @@ namespace cg = cooperative_groups;
 
 constexpr int PLAN_THREADS = 1024;
 
-__device__ __forceinline__ int pages_of(int tokens, int page_size) { return (int)(((long long)tokens + page_size - 1) / page_size); }
+// of tokens >= 0; both below 2^31, so that unsigned words hold the sum
+__device__ __forceinline__ int pages_of(int tokens, int page_size) { return (int)(((unsigned)tokens + (unsigned)page_size - 1u) / (unsigned)page_size); }
 
 // ---- eviction of the lowest pages ------------------------------------------------------------------
 // Score of a page: its tokens' weights added up in 64 bits, rounded to 32.  The candidates are the full pages with no token among the
@@ -106,8 +107,9 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
         if (TOGETHER) __syncthreads();
         else cluster.sync();
     };
-    float* s_w = reinterpret_cast<float*>(smem_raw);                              // [cap * ps] weights
-    int32_t* s_page = reinterpret_cast<int32_t*>(s_w + (size_t)cap * ps);         // [cap] table entries
+    const int stride = ps | 1;                   // of a page's weights: threads that add up a page each read different banks
+    float* s_w = reinterpret_cast<float*>(smem_raw);                              // [cap * stride] weights
+    int32_t* s_page = reinterpret_cast<int32_t*>(s_w + (size_t)cap * stride);     // [cap] table entries
     uint16_t* s_src = reinterpret_cast<uint16_t*>(s_page + cap);                  // [cap] pages that stay, in order
     uint32_t* s_key = reinterpret_cast<uint32_t*>(s_src + ((cap + 1) & ~1));      // [cap] scores (pages of one token: formed from s_w)
     pdl_wait();
@@ -115,22 +117,15 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     int32_t* stack;                              // the j-th page goes to stack[-j]
     CacheHeader* hdr = reinterpret_cast<CacheHeader*>(p.free_buf);
     if (TOGETHER) {
-        int takes[EV_MOST_CTAS], total = 0, bad = 0;
-        base = take = n = 0;
-        const int top = hdr->top;
-#pragma unroll
-        for (int i = 0; i < EV_MOST_CTAS; ++i) {
-            const int ni = i < p.S ? p.n_tokens[i] : 0;
-            const bool ok = ni >= 0 && pages_of(ni, ps) <= p.max_pages;
-            bad |= !ok;
-            takes[i] = ok ? pages_to_leave(p, ni) : 0;
-            base += i < s ? takes[i] : 0;
-            if (i == s) {
-                n = ni;
-                take = takes[i];
-            }
-            total += takes[i];
-        }
+        // every warp for itself, a lane for a sequence
+        const int top = hdr->top, ni = lane < p.S ? p.n_tokens[lane] : 0;
+        const bool ok = ni >= 0 && pages_of(ni, ps) <= p.max_pages;
+        const int leave = ok ? pages_to_leave(p, ni) : 0;
+        const bool bad = __any_sync(0xffffffffu, !ok);
+        const int total = __reduce_add_sync(0xffffffffu, leave);
+        base = __reduce_add_sync(0xffffffffu, lane < s ? leave : 0);
+        take = __shfl_sync(0xffffffffu, leave, s);
+        n = __shfl_sync(0xffffffffu, ni, s);
         const bool fits = top >= 0 && total <= p.num_pages - top;
         if (!fits) take = 0;
         cluster.sync();                          // all have read: now it may be written
@@ -164,13 +159,13 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
 #pragma unroll 8
     for (int i = tid; i < count; i += EV_THREADS) s_page[i] = table[first + i];
 #pragma unroll 8
-    for (int i = tid; i < count * ps; i += EV_THREADS) s_w[i] = weight[(size_t)first * ps + i];
+    for (int i = tid; i < count * ps; i += EV_THREADS) s_w[i + (stride - ps) * (int)((unsigned)i / (unsigned)ps)] = weight[(size_t)first * ps + i];
     for (int i = tid; i < 256 * EV_COPIES; i += EV_THREADS) s_count[i] = 0;
     __syncthreads();
     if (ps > 1) {
         for (int i = tid; i < count; i += EV_THREADS) {
             double sum = 0.0;
-            for (int j = 0; j < ps; ++j) sum += (double)s_w[i * ps + j];
+            for (int j = 0; j < ps; ++j) sum += (double)s_w[i * stride + j];
             s_key[i] = score_bits((float)sum);
         }
         __syncthreads();
@@ -283,8 +278,8 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
         if (to + k != first + src) table[to + k] = s_page[src];
     }
     for (int i = tid; i < stays * ps; i += EV_THREADS) {
-        const int k = i / ps, src = s_src[k];
-        if (to + k != first + src) weight[(size_t)to * ps + i] = s_w[src * ps + (i - k * ps)];
+        const int k = (int)((unsigned)i / (unsigned)ps), src = s_src[k];
+        if (to + k != first + src) weight[(size_t)to * ps + i] = s_w[src * stride + (i - k * ps)];
     }
     // no weight behind the last page
     for (int i = (live - take) * ps + c * EV_THREADS + tid; i < live * ps; i += C * EV_THREADS) weight[i] = 0.f;
@@ -510,7 +505,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) truncate_kernel(int n_drafted, c
 using namespace kvs;
 
 // A thread for a sequence, and a warp for its pages: few sequences need no large CTA
-static int plan_threads(int num_seqs) { return num_seqs <= 32 ? 128 : num_seqs <= 128 ? 256 : PLAN_THREADS; }
+static int plan_threads(int num_seqs, bool warps) {
+    const int want = warps ? num_seqs * 32 : num_seqs;
+    return want <= 128 ? 128 : want <= 256 ? 256 : want <= 512 ? 512 : PLAN_THREADS;
+}
 static bool cache_sizes_ok(int num_seqs, int page_size, int max_pages, int num_pages) {
     return num_seqs >= 0 && page_size > 0 && max_pages > 0 && num_pages > 0;
 }
@@ -521,7 +519,7 @@ extern "C" int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recen
     if (!cache_sizes_ok(num_seqs, page_size, max_pages, num_pages) || budget < 0 || keep_first < 0 || keep_recent < 0) return KVS_ERR_INVALID_ARG;
     if (num_seqs > (1 << 24) || (long long)max_pages * page_size > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
     // the cluster holds a sequence's weights, table and scores in shared memory
-    const long long page_bytes = 4ll * page_size + 6 + (page_size > 1 ? 4 : 0);
+    const long long page_bytes = 4ll * (page_size | 1) + 6 + (page_size > 1 ? 4 : 0);
     int C = 1;
     // more CTAs where a sequence has more than 1024 tokens for each and two CTAs an SM are not yet taken, or where it does not fit
     while (C < EV_MOST_CTAS && (((long long)max_pages * page_size > 1024ll * C && (long long)num_seqs * C < 148) ||
@@ -542,7 +540,7 @@ extern "C" int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recen
         return launch_clusters_after(evict_kernel<true>, dim3((unsigned)num_seqs), num_seqs, EV_THREADS, alone, st, p, max_pages);
     if (smem > EV_PLAIN_SMEM && cudaFuncSetAttribute(evict_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
         return cuda_refused();
-    const int rc = launch_after(evict_plan_kernel, 1, plan_threads(num_seqs), 0, st, p);
+    const int rc = launch_after(evict_plan_kernel, 1, plan_threads(num_seqs, false), 0, st, p);
     if (rc != KVS_OK) return rc;
     return launch_clusters_after(evict_kernel<false>, dim3((unsigned)(num_seqs * C)), C, EV_THREADS, smem, st, p, cap);
 }
@@ -565,7 +563,7 @@ extern "C" int kvs_cache_append_tokens(const void* k_new, const void* v_new, con
     if (num_seqs <= JOIN_SEQS && items <= 4 * JOIN_CTAS * JOIN_THREADS)
         return wide ? launch_clusters_after(join_together_kernel<uint4>, JOIN_CTAS, JOIN_CTAS, JOIN_THREADS, 0, st, p)
                     : launch_clusters_after(join_together_kernel<uint16_t>, JOIN_CTAS, JOIN_CTAS, JOIN_THREADS, 0, st, p);
-    const int rc = launch_after(join_plan_kernel, 1, plan_threads(num_seqs), 0, st, p);
+    const int rc = launch_after(join_plan_kernel, 1, plan_threads(num_seqs, true), 0, st, p);
     if (rc != KVS_OK) return rc;
     const unsigned grid = (unsigned)((items + 255) / 256 < 148 * 8 ? (items + 255) / 256 : 148 * 8);
     return wide ? launch_after(join_kernel<uint4>, grid, 256, 0, st, p) : launch_after(join_kernel<uint16_t>, grid, 256, 0, st, p);
@@ -579,6 +577,6 @@ extern "C" int kvs_cache_truncate(int n_drafted, const int32_t* n_accepted, int 
     if (!n_accepted || !block_table || !n_tokens || !free_list) return KVS_ERR_INVALID_ARG;
     if ((((uintptr_t)n_accepted | (uintptr_t)block_table | (uintptr_t)n_tokens | (uintptr_t)free_list | (uintptr_t)token_weight) & 3) != 0)
         return KVS_ERR_ALIGNMENT;
-    return launch_after(truncate_kernel, 1, plan_threads(num_seqs), 0, (cudaStream_t)stream, n_drafted, n_accepted, num_seqs, page_size, max_pages, num_pages, block_table,
+    return launch_after(truncate_kernel, 1, plan_threads(num_seqs, true), 0, (cudaStream_t)stream, n_drafted, n_accepted, num_seqs, page_size, max_pages, num_pages, block_table,
                         n_tokens, free_list, token_weight);
 }
