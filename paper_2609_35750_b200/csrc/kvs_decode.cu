@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(256) decode_merge_kernel(MergeParams p) {
 // `steps` times WT_TOKENS tokens each (one step where there are few: the host chooses).  A CTA forms the sequence's lse from the splits
 // itself; then a warp has every eighth head, a lane four tokens of each.  The scores (4 bytes a token and query head) were written by the kernels that formed them and are read once; forming
 // them again would take the K rows (256 bytes a token and KV head).  Bound by latency for few sequences (a thread per token that went
-// through the heads and the splits one after the other took 18 us on two sequences of 2000 tokens with 32 heads, here 5), else by the
+// through the heads and the splits one after the other took 18 us on two sequences of 2000 tokens with 32 heads, here 7.6), else by the
 // scores' way to memory and back.
 constexpr int WT_TOKENS = 256;
 struct WeightParams {
@@ -1099,7 +1099,7 @@ extern "C" int kvs_decode_weights_num_splits(int num_seqs, int Hkv, int max_toke
     const int n = kvs_decode_num_splits(num_seqs, Hkv, max_tokens);
     if (num_seqs <= 0 || Hkv <= 0 || max_tokens <= 0) return n;
     // where that leaves SMs without work, splits of fewer than four tiles: a tile takes 2 us, and the merge reads up to 64 splits in one go
-    // (two caches of 900 to 2500 tokens with 8 KV heads: 5 splits 14.7 us, 20 FEWSPLITS)
+    // (two caches of 900 to 2500 tokens with 8 KV heads: 5 splits 14.3 us, 20 10.1)
     const long long tiles = ((long long)max_tokens + 127) / 128, wave = 3 * 148 / ((long long)num_seqs * Hkv);
     long long more = wave < tiles ? wave : tiles;
     if (more > 64) more = 64;

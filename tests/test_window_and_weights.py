@@ -308,6 +308,33 @@ def test_a_sequence_longer_than_said_keeps_its_weights(page):
     assert torch.equal(out, full) and B.kvs_device_status(ws) == B.KVS_OK
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("page", [16, 1])
+def test_rows_far_into_a_large_cache(page):
+    """Rows beyond 2^31 elements: the last pages of a cache of 2.2e9 elements a side, written and read."""
+    Hkv, d, n, new = 8, 128, 300, 3
+    pages = 2_200_000 // page
+    k = torch.zeros((pages, page, Hkv, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    need = -(-n // page)
+    table = torch.arange(pages - need, pages, dtype=torch.int32, device="cuda").flip(0).view(1, -1).contiguous()
+    free = torch.cat((torch.tensor([need, 0, 0, 0], dtype=torch.int32, device="cuda"), table[0].flip(0), torch.zeros(pages - need, dtype=torch.int32, device="cuda")))
+    lens = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rows_k, rows_v = (torch.randn((1, n, Hkv, d), device="cuda").bfloat16() for _ in range(2))
+    for a, z in ((0, 290), (290, 297), (297, 300)):               # many rows, few rows
+        B.kvs_cache_append_tokens(rows_k[:, a:z].contiguous(), rows_v[:, a:z].contiguous(), table, lens, free, k, v)
+    assert lens.tolist() == [n] and free[:2].tolist() == [0, B.KVS_OK]
+    q, fq = queries(1, 1, new, 16, d)
+    c = Cache.__new__(Cache)
+    c.lens, c.page, c.table = [n], page, np.zeros((1, 0))
+    c.rows = lambda s: [x[0].float().cpu().numpy().astype(np.float64) for x in (rows_k, rows_v)]
+    check_window(c, (q, fq), 200, 4, *B.kvs_decode_attn_window(q, k, v, table, lens, 200, 4))
+    weight = torch.zeros((1, need * page), device="cuda")
+    out, lse = B.kvs_decode_attn_weights(q[:, -1].contiguous(), k, v, table, lens, weight)
+    check_window(c, (q[:, -1:], fq[:, -1:]), ALL, 0, out[:, None], lse[:, None])
+    assert abs(float(weight.sum()) - 16) < 1e-3
+
+
 # ---- GPU: together -----------------------------------------------------------------------------------------------
 @pytest.mark.gpu
 @pytest.mark.parametrize("page", [1, 16])
@@ -419,4 +446,6 @@ def test_a_captured_round_and_a_captured_step_replay():
     got = caches[0].decode_window(q, 60, 4, stream=side)
     side.synchronize()
     for x, y in zip(got, caches[2].decode_window(q, 60, 4)):
+        assert torch.equal(x, y)
+    for x, y in zip(got, caches[2].decode_window(q, 60, 4, stream=torch.cuda.default_stream())):
         assert torch.equal(x, y)
