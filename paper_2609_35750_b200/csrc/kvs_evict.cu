@@ -159,8 +159,13 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     float* weight = p.weight + (size_t)s * p.max_pages * ps;
 #pragma unroll 8
     for (int i = tid; i < count; i += EV_THREADS) s_page[i] = table[first + i];
+    if (stride == ps) {
 #pragma unroll 8
-    for (int i = tid; i < count * ps; i += EV_THREADS) s_w[i + (stride - ps) * (int)((unsigned)i / (unsigned)ps)] = weight[(size_t)first * ps + i];
+        for (int i = tid; i < count * ps; i += EV_THREADS) s_w[i] = weight[(size_t)first * ps + i];
+    } else {
+#pragma unroll 8
+        for (int i = tid; i < count * ps; i += EV_THREADS) s_w[i + (int)((unsigned)i / (unsigned)ps)] = weight[(size_t)first * ps + i];
+    }
     for (int i = tid; i < 256 * EV_COPIES; i += EV_THREADS) s_count[i] = 0;
     __syncthreads();
     if (ps > 1) {
@@ -172,7 +177,7 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
         __syncthreads();
     }
     auto key_of = [&](int i) { return ps == 1 ? score_bits(s_w[i]) : s_key[i]; };
-    auto candidate = [&](int i) { return first + i >= lo && first + i < hi; };
+    const int from = max(lo - first, 0), until = min(hi - first, count);          // this CTA's candidates
     // ---- the threshold: `take` candidates are below it, or on it and early ----
     uint32_t found = 0;
     int want = take;                                     // how many of those whose upper digits are `found`
@@ -180,9 +185,9 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
         const int shift = 24 - 8 * pass;
         int* hist = s_hist[pass & 1];
 #pragma unroll 4
-        for (int i = tid; i < count; i += EV_THREADS) {
+        for (int i = from + tid; i < until; i += EV_THREADS) {
             const uint32_t key = key_of(i);
-            if (candidate(i) && (pass == 0 || (key >> (shift + 8)) == (found >> (shift + 8))))
+            if (pass == 0 || (key >> (shift + 8)) == (found >> (shift + 8)))
                 atomicAdd(&s_count[((key >> shift) & 255u) * EV_COPIES + (lane & (EV_COPIES - 1))], 1);
         }
         __syncthreads();
@@ -221,12 +226,12 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     const int run = (count + EV_THREADS - 1) / EV_THREADS | 1;           // odd: the threads' pages lie in different banks
     const int a = min(tid * run, count), z = min(a + run, count);
     int under = 0, on = 0;
-    for (int i = a; i < z; ++i)
-        if (candidate(i)) {
-            const uint32_t key = key_of(i);
-            under += key < found;
-            on += key == found;
-        }
+#pragma unroll 4
+    for (int i = max(a, from); i < min(z, until); ++i) {
+        const uint32_t key = key_of(i);
+        under += key < found;
+        on += key == found;
+    }
     unsigned long long both;                             // the two counts side by side
     const unsigned long long before = block_prefix((unsigned long long)under << 32 | (unsigned)on, s_warp64, both);
     const int under_all = (int)(both >> 32), on_all = (int)(both & 0xffffffffu);
@@ -253,7 +258,7 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
     for (int i = a; i < z; ++i) {
         bool leaves = false;
         const int rank = under_before + min(on_before, of_equals);
-        if (candidate(i)) {
+        if (i >= from && i < until) {
             const uint32_t key = key_of(i);
             if (key < found) {
                 leaves = true;
@@ -278,7 +283,12 @@ __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int ca
         const int src = s_src[k];
         if (to + k != first + src) table[to + k] = s_page[src];
     }
-    for (int i = tid; i < stays * ps; i += EV_THREADS) {
+    if (ps == 1) {
+        for (int k = tid; k < stays; k += EV_THREADS) {
+            const int src = s_src[k];
+            if (to + k != first + src) weight[to + k] = s_w[src];
+        }
+    } else for (int i = tid; i < stays * ps; i += EV_THREADS) {
         const int k = (int)((unsigned)i / (unsigned)ps), src = s_src[k];
         if (to + k != first + src) weight[(size_t)to * ps + i] = s_w[src * stride + (i - k * ps)];
     }
