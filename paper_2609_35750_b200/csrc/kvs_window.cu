@@ -725,9 +725,12 @@ int window_groups(int G, int n_new) {
 template <int D, int COLS>
 int launch_window(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, long long most_tiles, bool pages, cudaStream_t st) {
     auto kern = pages ? decode_window_kernel<D, COLS, WIN_PAGES> : decode_window_kernel<D, COLS, WIN_ROWS>;
-    constexpr int bytes = WinSmem<D, COLS>::DYN_BYTES, resident = WinSmem<D, COLS>::CTAS;
+    constexpr int bytes = WinSmem<D, COLS>::DYN_BYTES;
+    // One wave.  Three CTAs fit on an SM with 16 columns; with TMA boxes two of them keep the memory busy and start and end sooner
+    // (64 sequences with a window of 4096 177 -> 172 us), rows need the third (40 sequences of one-token pages 45 -> 46 without it).
+    const int resident = pages ? 2 : WinSmem<D, COLS>::CTAS;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return cuda_refused();
-    const long long ctas = most_tiles < 148 * resident ? most_tiles : 148 * resident;        // one wave
+    const long long ctas = most_tiles < 148 * resident ? most_tiles : 148 * resident;
     return launch_after(kern, dim3((unsigned)(ctas < 1 ? 1 : ctas)), WinSmem<D, COLS>::THREADS, bytes, st, tk, tv, p);
 }
 template <int D>
