@@ -1083,6 +1083,8 @@ static int launch_decode(const DecodeParams& p, int G, const void* k_cache, cons
     const int merge_ctas = (m.rows + 7) / 8;
     if (!weight) return launch_after(p.nsplit <= 4 ? decode_merge_kernel<D, 4> : decode_merge_kernel<D, 16>, merge_ctas, 256, 0, st, m);
     const int most = min(p.score_stride, p.max_pages * p.page_size);
+    // longer runs of tokens where CTAs come in several waves: each forms the lse once (48 caches of up to 16000 tokens, 1 to 8 steps chosen by
+    // 3, 6, 12 and 24 CTAs an SM: 289, 283, 283, 286 us)
     int steps = 1;
     while (steps < 8 && (long long)p.S * ((most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps)) > 148 * 6) steps *= 2;
     const int chunks = (most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps);

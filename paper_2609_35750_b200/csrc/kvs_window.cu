@@ -16,7 +16,7 @@
 // head are on their way while the last one's result is written.  Fixed number of CTAs a sequence -> equal shares (us): one sequence with a
 // window of 256 14.1 -> 10.4, 16 of 500 to 6000 tokens with 5 new ones (with append and truncate) 70 -> 66, 24 of 3000 to 16000 the same.
 //
-// 64 sequences, 32 heads on 8, window 4096: 1.06 GB in 175 us, 6.1 TB/s (0.92 of the measured copy rate); nothing hidden, 48 sequences of up
+// 64 sequences, 32 heads on 8, window 4096: 1.06 GB in 172 us, 6.2 TB/s (0.94 of the measured copy rate); nothing hidden, 48 sequences of up
 // to 16000 tokens: 255 us, 0.99.  With 35 columns (5 new tokens, 7 heads a KV head) 0.47 GB in 96 us, 0.75: 10 us until the first tile is
 // through (launch, lengths, queries, first maxima), 12 between the first and the last CTA's end.
 //

@@ -210,6 +210,21 @@ def test_what_a_query_does_not_see_does_not_reach_it(Hq, Hkv, d, page, new, spli
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("S,new,Hq,Hkv", [(900, 1, 4, 2), (40, 30, 64, 1)])
+def test_more_sequences_and_groups_than_a_cta_has_threads(S, new, Hq, Hkv):
+    """The shares are found by several passes over the lengths; most sequences are empty or short, a few are long."""
+    rng = np.random.default_rng(S)
+    lens = np.where(rng.random(S) < 0.4, 0, rng.integers(1, 60, size=S))
+    lens[[0, S // 2, S - 1]] = [0, 400, 150]
+    c = Cache(11, lens.tolist(), 8, Hkv, 64)
+    q = queries(12, S, new, Hq, 64)
+    check_window(c, q, 100, 3, *B.kvs_decode_attn_window(q[0], *c.args(), 100, 3))
+    for n in (0, 33):                                           # nothing live anywhere; all alike
+        c = Cache(13, [n] * S, 8, Hkv, 64)
+        check_window(c, q, 20, 0, *B.kvs_decode_attn_window(q[0], *c.args(), 20))
+
+
+@pytest.mark.gpu
 def test_scores_far_apart_and_scale():
     """References that have to move by hundreds, in both directions, and an explicit scale."""
     c = Cache(5, [640, 333], 16, 2, 128)
