@@ -23,9 +23,10 @@
 // Rows reach shared memory as in kvs_decode_attn: pages of 8 to 128 tokens that tile 128 by one TMA box each, others by rows (K by
 // TMA gather4, V by cp.async).
 //
-// The softmax needs no maximum in most tiles: weights are taken against a reference per column in shared memory, a tile goes on
-// with it while no score is more than 2^8 above (one barrier that also takes a vote), and only else the columns' maxima are formed, the
-// reference moves and O^T is rescaled.
+// The softmax needs no maximum in most tiles: weights are taken against a reference per column in shared memory, which may lie anywhere
+// near the scores, because bf16 has the exponents of fp32 and a weight's 8 bits are the same at any size.  A tile goes on with it while no
+// score is more than 30 (in base-2 units) above, and a head begins with 0 where all scores of its first tile lie within 30 of that: one
+// barrier that also takes a vote.  Only else the columns' maxima are formed, the reference moves and O^T is rescaled.
 //
 // A tile in which some query does not see some key is masked by element.  V rows that no query sees are cleared in shared memory
 // (0 x NaN is NaN).  A V row that some see and others do not (the new tokens, the window's edge) may hold an infinity or a NaN: it is
@@ -39,6 +40,7 @@ namespace kvs {
 constexpr int WIN_PAGES = 1;         // one TMA box per page
 constexpr int WIN_ROWS = 2;          // K: TMA gather4; V: cp.async rows
 constexpr float WIN_UNSET = -1e30f;  // reference of a column that has seen no key yet: any score is far above it
+constexpr float WIN_NEAR = 30.f;     // weights of up to 2^30, sums and products of up to 2^30 x keys x |v|: far from what fp32 holds
 
 struct WindowEntry {                 // of the workspace, written by the first CTA
     long long before;                // tiles of the entries before it, for one KV head
@@ -273,7 +275,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         tmem_alloc(smem_u32(s_tmem), 4 * COLS);            // S^T twice and O^T, in a power of two
         tmem_relinquish();
     } else if (tid < COLS) {
-        s_ref[tid] = tid < start.u.cols ? WIN_UNSET : 0.f;       // columns past the last score 0 and never move
+        s_ref[tid] = 0.f;
     }
     tc_fence_before();
     __syncthreads();
@@ -537,9 +539,10 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     float sc[CH], ref[CH];
                     scores(col0 + c0, sc, ref);
 #pragma unroll
-                    for (int x = 0; x < CH; ++x) above |= sc[x] - ref[x] > 8.0f;
+                    for (int x = 0; x < CH; ++x) above |= first ? !(fabsf(sc[x]) <= WIN_NEAR) : sc[x] - ref[x] > WIN_NEAR;
                 }
-            const bool grow = group_any(1, WORKERS, above);
+            // the same decision in every thread.  In a head's first tile every column has to have seen a key: masked ones are looked at
+            const bool grow = group_any(1, WORKERS, above || (first && masked));
             if (it > 0) mbar_wait(bar_done, (it - 1) & 1, abort_flag, status);           // P^T is free, O^T up to date
             if (it > 0) tc_fence_after();
             if (to_patch) {                                     // the same decision in every thread
@@ -562,8 +565,10 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 named_bar_sync(1, WORKERS);
                 if (tid < COLS) {
                     const float top = fmaxf(fmaxf(s_wmax[tid], s_wmax[COLS + tid]), fmaxf(s_wmax[2 * COLS + tid], s_wmax[3 * COLS + tid]));
-                    const float ref = s_ref[tid], to = tid < cols && top - ref > 8.0f ? top : ref;
-                    s_alpha[tid] = fast_exp2(ref - to);
+                    const float ref = s_ref[tid];
+                    float to = ref;
+                    if (tid < cols) to = first ? (top > -INFINITY ? top : WIN_UNSET) : top - ref > WIN_NEAR ? top : ref;
+                    s_alpha[tid] = first ? 1.f : fast_exp2(ref - to);        // nothing has been added up before the first
                     s_ref[tid] = to;
                 }
                 named_bar_sync(1, WORKERS);
@@ -676,7 +681,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 ml[1] = flagged_sum(s_wmax[tid] + s_wmax[COLS + tid] + s_wmax[2 * COLS + tid] + s_wmax[3 * COLS + tid], *(volatile int32_t*)status);
             }
             if (left > 0) {
-                if (tid < COLS) s_ref[tid] = tid < c.u.cols ? WIN_UNSET : 0.f;
+                if (tid < COLS) s_ref[tid] = 0.f;
 #pragma unroll
                 for (int x = 0; x < WIDE; ++x) l_part[x] = 0.f;
                 named_bar_sync(1, WORKERS);                         // the references are read by all
