@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/DynamicTypes.h>
@@ -400,6 +401,13 @@ struct On {
         return t.device();
     }
 };
+// A call's workspace: the tensor given, or memory of torch's allocator without a tensor around it (which takes as long as the allocation)
+struct Scratch {
+    c10::DataPtr own;
+    void* p;
+    size_t n;
+    Scratch(PyObject* o, size_t need, const at::Tensor& like);
+};
 // address of a contiguous tensor of these sizes (-1: any) on that device
 void* checked(const at::Tensor& t, const char* name, at::ScalarType dtype, std::initializer_list<int64_t> sizes, const at::Tensor& like) {
     void* p = address(t, name, dtype);
@@ -409,6 +417,18 @@ void* checked(const at::Tensor& t, const char* name, at::ScalarType dtype, std::
     if (!same) value_error("%s has the wrong shape", name);
     if (t.device() != like.device()) value_error("%s is on another device", name);
     return p;
+}
+Scratch::Scratch(PyObject* o, size_t need, const at::Tensor& like) {
+    if (given(o)) {
+        const at::Tensor& t = tensor(o, "workspace");
+        p = checked(t, "workspace", U8, {-1}, like);
+        n = (size_t)t.numel();
+    } else {
+        Unlocked u;
+        own = c10::cuda::CUDACachingAllocator::get()->allocate(need);
+        p = own.get();
+        n = need;
+    }
 }
 // a size that the C interface takes as an int
 int small(int64_t n, const char* name) {
@@ -448,14 +468,13 @@ PyObject* decode_window(PyObject* const* a) {
     const int S = (int)c.S, n = small(new_, "q"), H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[12]), most = given_most ? given_most : (int)(c.P * c.page);
     int splits = whole(a[8]);
     if (splits <= 0) splits = lib.kvs_decode_window_num_splits(S, n, H, (int)c.Hkv, most, window, sinks);
-    const at::Tensor ws = given(a[11]) ? tensor(a[11], "workspace") : bytes(lib.kvs_decode_window_workspace_bytes(S, n, H, (int)c.Hkv, d, splits), q);
+    const Scratch ws(a[11], lib.kvs_decode_window_workspace_bytes(S, n, H, (int)c.Hkv, d, splits), q);
     const at::Tensor out = out_of(a[9], "out", q), lse = out_of(a[10], "lse", {c.S, new_, Hq}, q, F32);
-    void *po = checked(out, "out", BF16, {c.S, new_, Hq, c.d}, q), *pws = checked(ws, "workspace", U8, {-1}, q);
+    void* po = checked(out, "out", BF16, {c.S, new_, Hq, c.d}, q);
     float* pl = (float*)checked(lse, "lse", F32, {c.S, new_, Hq}, q);
-    const size_t wn = (size_t)ws.numel();
     call("kvs_decode_attn_window", [&] {
         return lib.kvs_decode_attn_window(pq, c.k, c.v, c.table, c.n, S, n, H, (int)c.Hkv, d, (int)c.page, (int)c.P, (int)c.pages, scale, window, sinks, splits, po,
-                                          pl, pws, wn, on.stream);
+                                          pl, ws.p, ws.n, on.stream);
     });
     return tuple({wrap(out, a[9]), wrap(lse, a[10])});
 }
@@ -473,14 +492,13 @@ PyObject* decode_weights(PyObject* const* a) {
     const int S = (int)c.S, H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[11]), most = given_most ? given_most : (int)(c.P * c.page);
     int splits = whole(a[7]);
     if (splits <= 0) splits = lib.kvs_decode_weights_num_splits(S, (int)c.Hkv, most);
-    const at::Tensor ws = given(a[10]) ? tensor(a[10], "workspace") : bytes(lib.kvs_decode_weights_workspace_bytes(S, H, d, splits, most), q);
+    const Scratch ws(a[10], lib.kvs_decode_weights_workspace_bytes(S, H, d, splits, most), q);
     const at::Tensor out = out_of(a[8], "out", q), lse = out_of(a[9], "lse", {c.S, Hq}, q, F32);
-    void *po = checked(out, "out", BF16, {c.S, Hq, c.d}, q), *pws = checked(ws, "workspace", U8, {-1}, q);
+    void* po = checked(out, "out", BF16, {c.S, Hq, c.d}, q);
     float* pl = (float*)checked(lse, "lse", F32, {c.S, Hq}, q);
-    const size_t wn = (size_t)ws.numel();
     call("kvs_decode_attn_weights", [&] {
         return lib.kvs_decode_attn_weights(pq, c.k, c.v, c.table, c.n, S, H, (int)c.Hkv, d, (int)c.page, (int)c.P, (int)c.pages, scale, splits, most, po, pl, pw,
-                                           pws, wn, on.stream);
+                                           ws.p, ws.n, on.stream);
     });
     return tuple({wrap(out, a[8]), wrap(lse, a[9])});
 }
