@@ -1100,10 +1100,12 @@ static size_t score_bytes(int num_seqs, int Hq, int max_tokens) { return sizeof(
 extern "C" int kvs_decode_weights_num_splits(int num_seqs, int Hkv, int max_tokens) {
     const int n = kvs_decode_num_splits(num_seqs, Hkv, max_tokens);
     if (num_seqs <= 0 || Hkv <= 0 || max_tokens <= 0) return n;
-    // where that leaves SMs without work, splits of fewer than four tiles: a tile takes 2 us, and the merge reads up to 64 splits in one go
-    // (two caches of 900 to 2500 tokens with 8 KV heads: 5 splits 14.3 us, 20 10.1)
-    const long long tiles = ((long long)max_tokens + 127) / 128, wave = 3 * 148 / ((long long)num_seqs * Hkv);
-    long long more = wave < tiles ? wave : tiles;
+    // where that leaves SMs without work, splits of fewer than four tiles, as many as make two CTAs an SM (the third starts 8 us late).
+    // 8 KV heads, sequences of 1250 to 2500 tokens (us): one 5 splits 14.2, 20 9.5; two 5 14.3, 10 11.5, 18 10.1, 20 10.7; four 5 15.4,
+    // 7 13.9, 9 12.3, 13 13.4
+    const long long tiles = ((long long)max_tokens + 127) / 128;
+    long long more = 2 * 148 / ((long long)num_seqs * Hkv);
+    if (more > tiles) more = tiles;
     if (more > 64) more = 64;
     return more > n ? (int)more : n;
 }
