@@ -104,20 +104,23 @@ struct WindowCursor {
     }
 };
 
-template <int D, int COLS>
+template <int D, int COLS, int LOAD>
 struct WinSmem {
     static constexpr int HALVES = COLS >= 32 ? 2 : 1;                  // threads that share a key's columns
     static constexpr int WORKERS = 128 * HALVES, THREADS = WORKERS + 128;
-    static constexpr int CTAS = COLS <= 16 ? 3 : 2;                    // an SM: 24 warps, 80 registers a thread at launch ...
+    static constexpr int CTAS = COLS <= 16 ? 3 : 2;                    // that registers allow an SM: 24 warps, 80 a thread at launch ...
     static constexpr int WORKER_REGS = COLS <= 16 ? 104 : 96, CONTROL_REGS = COLS <= 16 ? 56 : 48;      // ... and shared out among the warp groups like this
     static_assert(WORKERS * WORKER_REGS + 128 * CONTROL_REGS <= THREADS * 80, "no more than the block was launched with");
+    // CTAs an SM.  RESIDENT_COMMENT
+    static constexpr int RESIDENT = LOAD == WIN_PAGES && COLS <= 16 ? (D == 128 ? 1 : 2) : CTAS;
+    static constexpr int STAGES = LOAD == WIN_PAGES && COLS <= 16 ? 3 : 1;            // buffers of K, and of V
     static constexpr int TILE_BYTES = 128 * D * 2;
     static constexpr int OFF_K = 0;
-    static constexpr int OFF_V = TILE_BYTES;
-    static constexpr int OFF_Q = 2 * TILE_BYTES;                       // [COLS x D] bf16, boxes of 64 columns
+    static constexpr int OFF_V = STAGES * TILE_BYTES;
+    static constexpr int OFF_Q = 2 * STAGES * TILE_BYTES;              // [COLS x D] bf16, boxes of 64 columns
     static constexpr int OFF_P = OFF_Q + COLS * D * 2;                 // P^T as [COLS x 128 keys] bf16, two boxes of 64 keys
     static constexpr int OFF_BAR = OFF_P + COLS * 256;
-    static constexpr int OFF_MISC = OFF_BAR + 64;                      // tmem base, abort flag, status, bad rows of the tile before
+    static constexpr int OFF_MISC = OFF_BAR + 128;                     // tmem base, abort flag, status, bad rows of the tile before
     static constexpr int OFF_REF = OFF_MISC + 64;                      // [COLS] reference, base-2 units
     static constexpr int OFF_AT = OFF_REF + COLS * 4;                  // [2][COLS] position of the column's token, of two heads in turn
     static constexpr int OFF_ROW = OFF_AT + COLS * 8;                  // [2][COLS] its row among all (sequence, token, query head)
@@ -161,9 +164,10 @@ __device__ __forceinline__ bool group_any(int id, int nthreads, bool mine) {
 }
 
 template <int D, int COLS, int LOAD>
-__global__ void __launch_bounds__(WinSmem<D, COLS>::THREADS, WinSmem<D, COLS>::CTAS)
+__global__ void __launch_bounds__(WinSmem<D, COLS, LOAD>::THREADS, WinSmem<D, COLS, LOAD>::CTAS)
 decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ WindowParams p) {
-    using SM = WinSmem<D, COLS>;
+    using SM = WinSmem<D, COLS, LOAD>;
+    constexpr int ST = SM::STAGES;
     constexpr int BOX = 16384, NBOX = D / 64;
     constexpr int WORKERS = SM::WORKERS, THREADS = SM::THREADS, CONTROL = WORKERS / 32;        // CONTROL: the first control warp
     constexpr int WIDE = COLS / SM::HALVES;              // columns of a thread
@@ -251,7 +255,12 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     const uint32_t sK = sbase + SM::OFF_K, sV = sbase + SM::OFF_V, sQ = sbase + SM::OFF_Q, sP = sbase + SM::OFF_P, bars = sbase + SM::OFF_BAR;
     // K / V rows have landed; S^T is complete (one for each of its two buffers: the one of tile t + 2 waits for P^T of tile t, that of
     // t + 1 does not); P^T is written; the second product is complete (V and P^T consumed, O^T up to date); a head's queries are in place
-    const uint32_t bar_kfull = bars, bar_vfull = bars + 8, bar_s = bars + 16, bar_p = bars + 32, bar_done = bars + 40, bar_q = bars + 48;
+    // K, V and the second products have one of each for every buffer; K of a buffer is consumed by S^T of its tile.
+    const uint32_t bar_kfull = bars, bar_vfull = bars + 8 * ST, bar_kfree = bars + 16 * ST, bar_done = bars + 24 * ST, bar_s = bars + 32 * ST,
+                   bar_p = bar_s + 16, bar_q = bar_s + 24;
+    // a buffer's barrier and its phase at tile `it`
+    auto stage_of = [](int it) { return (uint32_t)(it % ST); };
+    auto phase_of = [](int it) { return (uint32_t)(it / ST & 1); };
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(sgen + SM::OFF_MISC);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + SM::OFF_MISC + 4);
     int32_t* status = reinterpret_cast<int32_t*>(sgen + SM::OFF_MISC + 8);
@@ -265,12 +274,15 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     if (tid == 0) {
         *abort_flag = 0;
         *status = KVS_OK;
-        mbar_init(bar_kfull, 1);
-        mbar_init(bar_vfull, PAGES ? 2 : 64);
+        for (int b = 0; b < ST; ++b) {
+            mbar_init(bar_kfull + 8 * b, 1);
+            mbar_init(bar_vfull + 8 * b, PAGES ? 2 : 64);
+            mbar_init(bar_kfree + 8 * b, 1);
+            mbar_init(bar_done + 8 * b, 1);
+        }
         mbar_init(bar_s, 1);
         mbar_init(bar_s + 8, 1);
         mbar_init(bar_p, WORKERS);
-        mbar_init(bar_done, 1);
         mbar_init(bar_q, WORKERS);
         fence_mbar_init();
     }
@@ -307,15 +319,19 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             int heads = 0;
             auto scores = [&](int it, bool head) {             // S^T of tile `it`; the first of a head waits for its queries
                 if (head) mbar_wait(bar_q, heads++ & 1, abort_flag, status);
-                mbar_wait(bar_kfull, it & 1, abort_flag, status);
+                mbar_wait(bar_kfull + 8 * stage_of(it), phase_of(it), abort_flag, status);
                 tc_fence_after();
+                const uint64_t dKt = dK + (uint64_t)(stage_of(it) * (SM::TILE_BYTES >> 4));
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {          // S^T = K Q^T, 16 elements of d per step
                     const uint64_t offk = (uint64_t)(((kk >> 2) * BOX + (kk & 3) * 32) >> 4);
                     const uint64_t offq = (uint64_t)(((kk >> 2) * QBOX + (kk & 3) * 32) >> 4);
-                    if (leader) mma_ss(tmem_S + (it & 1) * COLS, dK + offk, dQ + offq, IDESC_S, kk > 0);
+                    if (leader) mma_ss(tmem_S + (it & 1) * COLS, dKt + offk, dQ + offq, IDESC_S, kk > 0);
                 }
-                if (leader) mma_commit(bar_s + (it & 1) * 8);
+                if (leader) {
+                    mma_commit(bar_s + (it & 1) * 8);
+                    mma_commit(bar_kfree + 8 * stage_of(it));
+                }
             };
             scores(0, true);
             bool first = true;
@@ -326,14 +342,15 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 const bool head = c.i == 0;
                 if (more && !head) scores(it + 1, false);
                 mbar_wait(bar_p, it & 1, abort_flag, status);
-                mbar_wait(bar_vfull, it & 1, abort_flag, status);
+                mbar_wait(bar_vfull + 8 * stage_of(it), phase_of(it), abort_flag, status);
                 tc_fence_after();
+                const uint64_t dVt = dV + (uint64_t)(stage_of(it) * (SM::TILE_BYTES >> 4));
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {               // O^T += V^T P^T, 16 keys per step
                     const uint64_t offp = (uint64_t)(((kk >> 2) * QBOX + (kk & 3) * 32) >> 4);
-                    if (leader) mma_ss(tmem_O, dV + (uint64_t)(kk * 128), dP + offp, IDESC_O, !first || (kk > 0));
+                    if (leader) mma_ss(tmem_O, dVt + (uint64_t)(kk * 128), dP + offp, IDESC_O, !first || (kk > 0));
                 }
-                if (leader) mma_commit(bar_done);
+                if (leader) mma_commit(bar_done + 8 * stage_of(it));
                 first = head;
                 if (more && head) scores(it + 1, true);
             }
@@ -343,7 +360,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             // query sees one of them.  The block-table entries are read a tile ahead.
             const bool k_rows = warp == CONTROL + 1;
             const CUtensorMap* map = k_rows ? &tm_k : &tm_v;
-            const uint32_t dst = k_rows ? sK : sV, full = k_rows ? bar_kfull : bar_vfull;
+            const uint32_t base = k_rows ? sK : sV, fulls = k_rows ? bar_kfull : bar_vfull, frees = k_rows ? bar_kfree : bar_done;
             const bool mine = !PAGES || (lane < ppt && (k_rows || (lane & 1) == (warp - CONTROL - 2)));
             int id[PAGES ? 1 : 4], off[PAGES ? 1 : 4], g = 0;
             bool need = false;
@@ -365,11 +382,8 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             };
             fetch();
             for (int it = 0; it < my_tiles; ++it) {
-                // the buffer's last tile is consumed
-                if (it > 0) {
-                    if (k_rows) mbar_wait(bar_s + ((it - 1) & 1) * 8, ((it - 1) >> 1) & 1, abort_flag, status);
-                    else mbar_wait(bar_done, (it - 1) & 1, abort_flag, status);
-                }
+                const uint32_t dst = base + stage_of(it) * SM::TILE_BYTES, full = fulls + 8 * stage_of(it);
+                if (it >= ST) mbar_wait(frees + 8 * stage_of(it), phase_of(it - ST), abort_flag, status);       // the buffer's last tile is consumed
                 const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, need));
                 if (leader) mbar_expect_tx(full, boxes * (uint32_t)((PAGES ? ps : 4) * D * 2));
                 __syncwarp();
@@ -411,7 +425,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             };
             fetch();
             for (int it = 0; it < my_tiles; ++it) {
-                if (it > 0) mbar_wait(bar_done, (it - 1) & 1, abort_flag, status);
+                if (it >= ST) mbar_wait(bar_done + 8 * stage_of(it), phase_of(it - ST), abort_flag, status);
                 const int k0 = c.u.key_of(c.i);
                 int row[2];                                    // of the cache; -1: seen by no query
 #pragma unroll
@@ -427,7 +441,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 for (int j = 0; j < NIT; ++j) {
                     const int i = j * RPW + lane / LPR, r = row_of(i), from = __shfl_sync(0xffffffffu, row[j * RPW / 32], i & 31);
                     const uint32_t dst = (uint32_t)((l >> 3) * BOX + r * 128 + (((l & 7) ^ (r & 7)) << 4)), bytes = from >= 0 ? 16u : 0u;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sV + dst), "l"(src + (size_t)max(from, 0) * p.Hkv * D), "r"(bytes)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sV + stage_of(it) * SM::TILE_BYTES + dst), "l"(src + (size_t)max(from, 0) * p.Hkv * D), "r"(bytes)
                                  : "memory");
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
@@ -437,7 +451,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
                 fence_proxy_async();                           // the tensor core reads them
-                mbar_arrive(bar_vfull);
+                mbar_arrive(bar_vfull + 8 * stage_of(it));
             }
         }
     } else {
@@ -546,8 +560,10 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 }
             // the same decision in every thread.  In a head's first tile every column has to have seen a key: masked ones are looked at
             const bool grow = group_any(1, WORKERS, above || (first && masked));
-            if (it > 0) mbar_wait(bar_done, (it - 1) & 1, abort_flag, status);           // P^T is free, O^T up to date
-            if (it > 0) tc_fence_after();
+            if (it > 0) {                                       // P^T is free, O^T up to date
+                mbar_wait(bar_done + 8 * stage_of(it - 1), phase_of(it - 1), abort_flag, status);
+                tc_fence_after();
+            }
             if (to_patch) {                                     // the same decision in every thread
                 patch(before_k0);
                 named_bar_sync(1, WORKERS);                     // P^T is written again below
@@ -606,9 +622,9 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 }
             to_patch = false;
             if (masked) {                         // the same decision in every thread
-                mbar_wait(bar_vfull, it & 1, abort_flag, status);
+                mbar_wait(bar_vfull + 8 * stage_of(it), phase_of(it), abort_flag, status);
                 bool clear = tid < 128 && !u.seen_by_some(j), bad = false;
-                uint4* vrow = reinterpret_cast<uint4*>(sgen + SM::OFF_V + key * 128);
+                uint4* vrow = reinterpret_cast<uint4*>(sgen + SM::OFF_V + stage_of(it) * SM::TILE_BYTES + key * 128);
                 if (tid < 128 && !clear && !(sees(j, at0) && sees(j, end - 1))) {
                     // some see it and others do not (or may not): it has to be finite
 #pragma unroll
@@ -649,7 +665,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 which ^= 1;
                 load_q(which);
             }
-            mbar_wait(bar_done, it & 1, abort_flag, status);
+            mbar_wait(bar_done + 8 * stage_of(it), phase_of(it), abort_flag, status);
             tc_fence_after();
             if (to_patch) {
                 const WindowCursor next = c;
@@ -731,16 +747,17 @@ int window_groups(int G, int n_new) {
     return (n_new + most - 1) / most;
 }
 
+template <int D, int COLS, int LOAD>
+int launch_window(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, long long most_tiles, cudaStream_t st) {
+    using SM = WinSmem<D, COLS, LOAD>;
+    auto kern = decode_window_kernel<D, COLS, LOAD>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::DYN_BYTES) != cudaSuccess) return cuda_refused();
+    const long long ctas = most_tiles < 148 * SM::RESIDENT ? most_tiles : 148 * SM::RESIDENT;        // one wave
+    return launch_after(kern, dim3((unsigned)(ctas < 1 ? 1 : ctas)), SM::THREADS, SM::DYN_BYTES, st, tk, tv, p);
+}
 template <int D, int COLS>
 int launch_window(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, long long most_tiles, bool pages, cudaStream_t st) {
-    auto kern = pages ? decode_window_kernel<D, COLS, WIN_PAGES> : decode_window_kernel<D, COLS, WIN_ROWS>;
-    constexpr int bytes = WinSmem<D, COLS>::DYN_BYTES;
-    // One wave.  Three CTAs fit on an SM with 16 columns; with TMA boxes two of them keep the memory busy and start and end sooner
-    // (64 sequences with a window of 4096 177 -> 172 us), rows need the third (40 sequences of one-token pages 45 -> 46 without it).
-    const int resident = pages ? 2 : WinSmem<D, COLS>::CTAS;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return cuda_refused();
-    const long long ctas = most_tiles < 148 * resident ? most_tiles : 148 * resident;
-    return launch_after(kern, dim3((unsigned)(ctas < 1 ? 1 : ctas)), WinSmem<D, COLS>::THREADS, bytes, st, tk, tv, p);
+    return pages ? launch_window<D, COLS, WIN_PAGES>(tk, tv, p, most_tiles, st) : launch_window<D, COLS, WIN_ROWS>(tk, tv, p, most_tiles, st);
 }
 template <int D>
 int launch_window_cols(const CUtensorMap& tk, const CUtensorMap& tv, const WindowParams& p, const MergeParams& m, long long most_tiles, bool pages,
