@@ -111,9 +111,15 @@ struct WinSmem {
     static constexpr int CTAS = COLS <= 16 ? 3 : 2;                    // that registers allow an SM: 24 warps, 80 a thread at launch ...
     static constexpr int WORKER_REGS = COLS <= 16 ? 104 : 96, CONTROL_REGS = COLS <= 16 ? 56 : 48;      // ... and shared out among the warp groups like this
     static_assert(WORKERS * WORKER_REGS + 128 * CONTROL_REGS <= THREADS * 80, "no more than the block was launched with");
-    // CTAs an SM.  RESIDENT_COMMENT
+    // CTAs an SM, and buffers of K and of V.  With TMA boxes and up to 16 columns one CTA with three of each keeps as much in flight as three with
+    // one, and an SM's second CTA starts 5 us after its first, the third 8 (us, d = 128: 64 sequences with a window of 4096 three CTAs 177, two
+    // 172.6, one 167.4; 8 of 1000 to 2000 tokens 20.2, 20.2, 18.4).  Heads of 64 have tiles of half the bytes: two CTAs with two of each (64 of
+    // 8000 to 16000 tokens, 16 heads on 4: one with three 181, two with three 171, three with one 170, two with two 164; with 20 columns two with
+    // one 182, two with two 171; one-token pages, three with one 176, three with two 159).  From 17 columns on the
+    // softmax of one CTA is the bound (64 of 1000 to 2000 tokens with 20 columns: two with one 87, one with three 101), and rows come too
+    // slowly by the warps of one (82 -> 141).
     static constexpr int RESIDENT = LOAD == WIN_PAGES && COLS <= 16 ? (D == 128 ? 1 : 2) : CTAS;
-    static constexpr int STAGES = LOAD == WIN_PAGES && COLS <= 16 ? 3 : 1;            // buffers of K, and of V
+    static constexpr int STAGES = D == 64 ? 2 : LOAD == WIN_PAGES && COLS <= 16 ? 3 : 1;
     static constexpr int TILE_BYTES = 128 * D * 2;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_V = STAGES * TILE_BYTES;
