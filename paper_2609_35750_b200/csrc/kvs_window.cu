@@ -107,10 +107,15 @@ struct WindowCursor {
 template <int D, int COLS, int LOAD>
 struct WinSmem {
     static constexpr int HALVES = COLS >= 32 ? 2 : 1;                  // threads that share a key's columns
-    static constexpr int WORKERS = 128 * HALVES, THREADS = WORKERS + 128;
-    static constexpr int CTAS = COLS <= 16 ? 3 : 2;                    // that registers allow an SM: 24 warps, 80 a thread at launch ...
-    static constexpr int WORKER_REGS = COLS <= 16 ? 104 : 96, CONTROL_REGS = COLS <= 16 ? 56 : 48;      // ... and shared out among the warp groups like this
-    static_assert(WORKERS * WORKER_REGS + 128 * CONTROL_REGS <= THREADS * 80, "no more than the block was launched with");
+    // warps beside them: one issues the products, the others load.  Issuing a tile's 64 gathers of K takes a warp 5600 clocks, twice the tile's
+    // share of the memory's time: rows of 256 bytes are loaded by seven warps of one CTA where registers allow it
+    static constexpr bool MANY = LOAD == WIN_ROWS && COLS <= 16 && D == 128;
+    static constexpr int K_WARPS = MANY ? 3 : 1, V_WARPS = MANY ? 4 : 2, CONTROLS = 32 * (1 + K_WARPS + V_WARPS);
+    static constexpr int WORKERS = 128 * HALVES, THREADS = WORKERS + CONTROLS;
+    static constexpr int CTAS = COLS <= 16 && !MANY ? 3 : 2;           // that registers allow an SM: 24 warps, 80 a thread at launch ...
+    static constexpr int WORKER_REGS = COLS <= 16 ? 104 : 96;          // ... and shared out among the warp groups like this
+    static constexpr int CONTROL_REGS = MANY ? 64 : COLS <= 16 ? 56 : 48;
+    static_assert(WORKERS * WORKER_REGS + CONTROLS * CONTROL_REGS <= THREADS * 80, "no more than the block was launched with");
     // CTAs an SM, and buffers of K and of V.  With TMA boxes and up to 16 columns one CTA with three of each keeps as much in flight as three with
     // one, and an SM's second CTA starts 5 us after its first, the third 8 (us, d = 128: 64 sequences with a window of 4096 three CTAs 177, two
     // 172.6, one 167.4; 8 of 1000 to 2000 tokens 20.2, 20.2, 18.4).  Heads of 64 have tiles of half the bytes: two CTAs with two of each (64 of
@@ -118,8 +123,8 @@ struct WinSmem {
     // one 182, two with two 171; one-token pages, three with one 176, three with two 159).  From 17 columns on the
     // softmax of one CTA is the bound (64 of 1000 to 2000 tokens with 20 columns: two with one 87, one with three 101), and rows come too
     // slowly by the warps of one (82 -> 141).
-    static constexpr int RESIDENT = LOAD == WIN_PAGES && COLS <= 16 ? (D == 128 ? 1 : 2) : CTAS;
-    static constexpr int STAGES = D == 64 ? 2 : LOAD == WIN_PAGES && COLS <= 16 ? 3 : 1;
+    static constexpr int RESIDENT = MANY ? 1 : LOAD == WIN_PAGES && COLS <= 16 ? (D == 128 ? 1 : 2) : CTAS;
+    static constexpr int STAGES = D == 64 ? 2 : COLS <= 16 ? 3 : 1;
     static constexpr int TILE_BYTES = 128 * D * 2;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_V = STAGES * TILE_BYTES;
@@ -281,8 +286,8 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         *abort_flag = 0;
         *status = KVS_OK;
         for (int b = 0; b < ST; ++b) {
-            mbar_init(bar_kfull + 8 * b, 1);
-            mbar_init(bar_vfull + 8 * b, PAGES ? 2 : 64);
+            mbar_init(bar_kfull + 8 * b, SM::K_WARPS);
+            mbar_init(bar_vfull + 8 * b, PAGES ? 2 : 32 * SM::V_WARPS);
             mbar_init(bar_kfree + 8 * b, 1);
             mbar_init(bar_done + 8 * b, 1);
         }
@@ -314,7 +319,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     };
 
     if (warp >= CONTROL) {
-        // ================= control warps: one issues the products, one loads K, two load V =================
+        // ================= control warps: one issues the products, the others load K and V =================
         reg_dec<SM::CONTROL_REGS>();
         const bool leader = elect_one();
         const int ppt = PAGES ? 128 / ps : 0;                  // pages per tile
@@ -360,14 +365,14 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 first = head;
                 if (more && head) scores(it + 1, true);
             }
-        } else if (PAGES || warp == CONTROL + 1) {
+        } else if (PAGES || warp <= CONTROL + SM::K_WARPS) {
             // TMA.  PAGES: lane i has page i of the tile, if some query sees a row of it (of V every second page is the other warp's).
             // ROWS: K alone, lane L has the rows 4 L .. 4 L + 3 (rows past the end repeat the last one: their scores are masked), if some
-            // query sees one of them.  The block-table entries are read a tile ahead.
-            const bool k_rows = warp == CONTROL + 1;
+            // query sees one of them, and if they are this warp's.  The block-table entries are read a tile ahead.
+            const bool k_rows = !PAGES || warp == CONTROL + 1;
             const CUtensorMap* map = k_rows ? &tm_k : &tm_v;
             const uint32_t base = k_rows ? sK : sV, fulls = k_rows ? bar_kfull : bar_vfull, frees = k_rows ? bar_kfree : bar_done;
-            const bool mine = !PAGES || (lane < ppt && (k_rows || (lane & 1) == (warp - CONTROL - 2)));
+            const bool mine = PAGES ? lane < ppt && (k_rows || (lane & 1) == (warp - CONTROL - 2)) : lane % SM::K_WARPS == warp - CONTROL - 1;
             int id[PAGES ? 1 : 4], off[PAGES ? 1 : 4], g = 0;
             bool need = false;
             auto fetch = [&]() {                               // of the tile at the cursor
@@ -414,16 +419,16 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 }
             }
         } else {
-            // V by rows: 16 bytes of a row a lane, LPR lanes a row, two warps; rows that no query sees are filled with zeros.  A lane has the
-            // block-table entries of two of its warp's 64 rows, read a tile ahead, and hands their rows of the cache to the lanes that copy.
-            constexpr int LPR = D / 8, RPW = 32 / LPR, NIT = 64 / RPW;
-            const int part = warp - CONTROL - 2, l = lane % LPR;
-            auto row_of = [&](int i) { return i / RPW * (2 * RPW) + part * RPW + i % RPW; };         // the warp's i-th row in the tile
-            int id[2];
+            // V by rows: 16 bytes of a row a lane, LPR lanes a row; rows that no query sees are filled with zeros.  A lane has the block-table
+            // entries of IDS of its warp's rows, read a tile ahead, and hands their rows of the cache to the lanes that copy.
+            constexpr int LPR = D / 8, RPW = 32 / LPR, ROWS = 128 / SM::V_WARPS, IDS = ROWS / 32, NIT = ROWS / RPW;
+            const int part = warp - CONTROL - 1 - SM::K_WARPS, l = lane % LPR;
+            auto row_of = [&](int i) { return i / RPW * (SM::V_WARPS * RPW) + part * RPW + i % RPW; };         // the warp's i-th row in the tile
+            int id[IDS];
             auto fetch = [&]() {
                 const int32_t* bt = p.block_table + (size_t)c.u.s * p.max_pages;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < IDS; ++h) {
                     int en, o;
                     split_token(min(c.u.key_of(c.i) + row_of(lane + 32 * h), c.u.end - 1), en, o);
                     id[h] = bt[en];
@@ -433,9 +438,9 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             for (int it = 0; it < my_tiles; ++it) {
                 if (it >= ST) mbar_wait(bar_done + 8 * stage_of(it), phase_of(it - ST), abort_flag, status);
                 const int k0 = c.u.key_of(c.i);
-                int row[2];                                    // of the cache; -1: seen by no query
+                int row[IDS];                                    // of the cache; -1: seen by no query
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < IDS; ++h) {
                     const int k = k0 + row_of(lane + 32 * h);
                     int en, o;
                     split_token(min(k, c.u.end - 1), en, o);
