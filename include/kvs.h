@@ -421,7 +421,7 @@ int kvs_decode_attn_window(const void* q, const void* k_cache, const void* v_cac
 /*
  * kvs_decode_attn that also accumulates attention weights: token_weight[s, j] += sum over query heads h of
  * exp(scale * q[s,h].k_j - lse[s,h]) for every live token j (fp32 [num_seqs, max_pages * page_size], in the order of the live
- * cache, as kvs_cache_evict_lowest takes it), the heads added in order.  max_tokens: no sequence has more live tokens; the workspace has
+ * cache, as kvs_cache_evict_lowest takes it), the heads added in a fixed order.  max_tokens: no sequence has more live tokens; the workspace has
  * room for that many scores per query head.  A longer sequence gets its attention, keeps its weights, and sets KVS_ERR_INVALID_ARG in
  * the workspace's status word.  num_splits as in kvs_decode_attn; kvs_decode_weights_num_splits gives one that fills the GPU.  Hq <= 8192.  Everything else as in kvs_decode_attn.
  */
@@ -444,7 +444,8 @@ int kvs_decode_attn_weights(const void* q, const void* k_cache, const void* v_ca
  * what the trainer's evict_at needs: the caller knows which tokens the slots held.  n_evicted: int32 [num_seqs], pages.
  * n_tokens of a sequence that its table cannot hold: KVS_ERR_INVALID_ARG in the cache status word, that sequence stays as it is.
  * A sequence's weights, table and scores have to fit into the shared memory of a cluster: about 150000 tokens with pages of one or two
- * tokens, 340000 with pages of 16; larger max_pages * page_size return KVS_ERR_UNSUPPORTED.
+ * tokens, 340000 with pages of 16; larger max_pages * page_size return KVS_ERR_UNSUPPORTED, as do here and in the two calls below
+ * tables of 2^31 entries or more (num_seqs * max_pages).
  * kvs_cache_evict does not know of token_weight: a cache with weights is not evicted by ranges.
  */
 int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recent,

@@ -520,6 +520,10 @@ static int plan_threads(int num_seqs, bool warps) {
     const int want = warps ? num_seqs * 32 : num_seqs;
     return want <= 128 ? 128 : want <= 256 ? 256 : want <= 512 ? 512 : PLAN_THREADS;
 }
+// Tokens of a sequence and pages of all sequences are counted in 32 bits: a sum that wrapped would pass for one that fits the stack
+static bool counts_fit(int num_seqs, int page_size, int max_pages) {
+    return (long long)max_pages * page_size <= 0x7fffffffLL && (long long)num_seqs * max_pages <= 0x7fffffffLL;
+}
 static bool cache_sizes_ok(int num_seqs, int page_size, int max_pages, int num_pages) {
     return num_seqs >= 0 && page_size > 0 && max_pages > 0 && num_pages > 0;
 }
@@ -528,7 +532,7 @@ extern "C" int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recen
                                       int32_t* block_table, int32_t* n_tokens, int32_t* free_list, float* token_weight, int32_t* evicted,
                                       int32_t* n_evicted, kvs_stream_t stream) {
     if (!cache_sizes_ok(num_seqs, page_size, max_pages, num_pages) || budget < 0 || keep_first < 0 || keep_recent < 0) return KVS_ERR_INVALID_ARG;
-    if (num_seqs > (1 << 24) || (long long)max_pages * page_size > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
+    if (num_seqs > (1 << 24) || !counts_fit(num_seqs, page_size, max_pages)) return KVS_ERR_UNSUPPORTED;
     // the cluster holds a sequence's weights, table and scores in shared memory
     const long long page_bytes = 4ll * (page_size | 1) + 6 + (page_size > 1 ? 4 : 0);
     int C = 1;
@@ -560,7 +564,7 @@ extern "C" int kvs_cache_append_tokens(const void* k_new, const void* v_new, con
                                        int page_size, int max_pages, int num_pages, int32_t* block_table, int32_t* n_tokens, int32_t* free_list,
                                        void* k_cache, void* v_cache, kvs_stream_t stream) {
     if (!cache_sizes_ok(num_seqs, page_size, max_pages, num_pages) || n_new < 0 || Hkv <= 0 || head_dim <= 0) return KVS_ERR_INVALID_ARG;
-    if ((long long)max_pages * page_size > 0x7fffffffLL || (long long)Hkv * head_dim > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
+    if (!counts_fit(num_seqs, page_size, max_pages) || (long long)Hkv * head_dim > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
     if (num_seqs == 0 || n_new == 0) return KVS_OK;
     if (!k_new || !v_new || !block_table || !n_tokens || !free_list || !k_cache || !v_cache) return KVS_ERR_INVALID_ARG;
     const uintptr_t rows = (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)k_cache | (uintptr_t)v_cache;
@@ -584,7 +588,7 @@ extern "C" int kvs_cache_append_tokens(const void* k_new, const void* v_new, con
 extern "C" int kvs_cache_truncate(int n_drafted, const int32_t* n_accepted, int num_seqs, int page_size, int max_pages, int num_pages,
                                   const int32_t* block_table, int32_t* n_tokens, int32_t* free_list, float* token_weight, kvs_stream_t stream) {
     if (!cache_sizes_ok(num_seqs, page_size, max_pages, num_pages) || n_drafted < 0) return KVS_ERR_INVALID_ARG;
-    if ((long long)max_pages * page_size > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
+    if (!counts_fit(num_seqs, page_size, max_pages)) return KVS_ERR_UNSUPPORTED;
     if (num_seqs == 0 || n_drafted == 0) return KVS_OK;
     if (!n_accepted || !block_table || !n_tokens || !free_list) return KVS_ERR_INVALID_ARG;
     if ((((uintptr_t)n_accepted | (uintptr_t)block_table | (uintptr_t)n_tokens | (uintptr_t)free_list | (uintptr_t)token_weight) & 3) != 0)

@@ -83,6 +83,14 @@ def test_host_refusals_need_no_gpu(lib):
     assert tr(S=0) == tr(drafted=0) == B.KVS_OK
 
 
+def test_tables_of_more_entries_than_32_bits_count_are_refused(lib):
+    p = 1 << 20                                                # an address that is never followed
+    for S, P in ((1 << 16, 1 << 15), (1 << 20, 1 << 12), (1 << 24, 128)):
+        assert lib.kvs_cache_evict_lowest(1, 0, 0, S, 1, P, 4, p, p, p, p, None, p, None) == B.KVS_ERR_UNSUPPORTED
+        assert lib.kvs_cache_append_tokens(p, p, None, S, 1, 1, 64, 1, P, 4, p, p, p, p, p, None) == B.KVS_ERR_UNSUPPORTED
+        assert lib.kvs_cache_truncate(1, p, S, 1, P, 4, p, p, p, None, None) == B.KVS_ERR_UNSUPPORTED
+
+
 def test_host_tensors_are_refused(lib):
     i, f = torch.zeros((1, 4), dtype=torch.int32), torch.zeros((1, 4))
     with pytest.raises(ValueError, match="CUDA"):
