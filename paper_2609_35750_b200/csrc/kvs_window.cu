@@ -7,8 +7,9 @@
 //   O^T [d x N]       += V^T [d x 128 keys] P^T     A = V tile read MN-major, B = P^T  (d = 64: rows 64 .. 127 repeat rows 0 .. 63)
 // Four softmax warps (a thread has a key of S^T and a column d of O^T; from 17 columns on eight, which halve the columns), a warp that
 // issues the products, one that loads K and two that load V (by one control warp a tile took 5900 clocks, 1300 of them to issue its 16 TMA
-// instructions for K, as many for V).  S^T of tile t + 1 is formed while tile t is in work, K of tile t + 2 is asked for as soon as
-// that is complete, V of tile t + 1 as soon as the second product of tile t is; two or three CTAs an SM overlap what is left of the chain.
+// instructions for K, as many for V; rows of 256 bytes take seven).  S^T of tile t + 1 is formed while tile t is in work; with a single buffer K
+// of tile t + 2 is asked for as soon as that is complete, V of tile t + 1 as soon as the second product of tile t is, and two CTAs an SM
+// overlap what is left of the chain; up to 16 columns two or three buffers do that (see `STAGES`).
 //
 // Every CTA has an equal share of all tiles: the tiles of (sequence and group of new tokens, KV head) follow one another, CTA c has
 // tiles c share .. (c + 1) share - 1 of them, whose heads end where they end.  Lengths are ragged and known on the device alone, so every
@@ -16,9 +17,9 @@
 // head are on their way while the last one's result is written.  Fixed number of CTAs a sequence -> equal shares (us): one sequence with a
 // window of 256 14.1 -> 10.4, 16 of 500 to 6000 tokens with 5 new ones (with append and truncate) 70 -> 66, 24 of 3000 to 16000 the same.
 //
-// 64 sequences, 32 heads on 8, window 4096: 1.06 GB in 172 us, 6.2 TB/s (0.94 of the measured copy rate); nothing hidden, 48 sequences of up
-// to 16000 tokens: 255 us, 0.99.  With 35 columns (5 new tokens, 7 heads a KV head) 0.47 GB in 96 us, 0.75: 10 us until the first tile is
-// through (launch, lengths, queries, first maxima), 12 between the first and the last CTA's end.
+// 64 sequences, 32 heads on 8, window 4096: 1.06 GB in 170 us, 6.2 TB/s (0.95 of the measured copy rate); nothing hidden, 48 sequences of up
+// to 16000 tokens: 253 us, 0.99; 64 of 7000 one-token pages 152 us, 0.9.  With 35 columns (5 new tokens, 7 heads a KV head) 0.47 GB in 93 us,
+// 0.77: 10 us until the first tile is through (launch, lengths, queries, first maxima), 12 between the first and the last CTA's end.
 //
 // Rows reach shared memory as in kvs_decode_attn: pages of 8 to 128 tokens that tile 128 by one TMA box each, others by rows (K by
 // TMA gather4, V by cp.async).
