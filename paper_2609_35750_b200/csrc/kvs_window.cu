@@ -18,8 +18,8 @@
 // window of 256 14.1 -> 10.4, 16 of 500 to 6000 tokens with 5 new ones (with append and truncate) 70 -> 66, 24 of 3000 to 16000 the same.
 //
 // 64 sequences, 32 heads on 8, window 4096: 1.06 GB in 170 us, 6.2 TB/s (0.95 of the measured copy rate); nothing hidden, 48 sequences of up
-// to 16000 tokens: 253 us, 0.99; 64 of 7000 one-token pages 152 us, 0.9.  With 35 columns (5 new tokens, 7 heads a KV head) 0.47 GB in 93 us,
-// 0.77: 10 us until the first tile is through (launch, lengths, queries, first maxima), 12 between the first and the last CTA's end.
+// to 16000 tokens: 253 us, 0.99; 64 of 7000 one-token pages 152 us, 0.9.  With 35 columns (5 new tokens, 7 heads a KV head) 0.47 GB in 91 us,
+// 0.79: 10 us until the first tile is through (launch, lengths, queries, first maxima), 12 between the first and the last CTA's end.
 //
 // Rows reach shared memory as in kvs_decode_attn: pages of 8 to 128 tokens that tile 128 by one TMA box each, others by rows (K by
 // TMA gather4, V by cp.async).
@@ -192,12 +192,50 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     __shared__ int s_most, s_entry;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int ps = p.page_size, G = p.G, E = p.S * p.groups;
-    if (tid == 0) s_most = 0;
-    __syncthreads();
+    if (E > 32) {
+        if (tid == 0) s_most = 0;
+        __syncthreads();
+    }
     pdl_wait();
     // ---- this CTA's share ----
-    long long share, at, all;
-    {
+    long long share, at, all, entry_before;
+    int entry;
+    // tiles of a CTA: not so few that a head is cut into more parts than there is room for: the first may be cut anywhere.
+    // The second CTA of an SM starts 5 us after the first, which is worth two tiles: up to three tiles an SM are one CTA's (4 sequences of
+    // 1000 to 2000 tokens, 392 tiles, 15.7 -> 14.0 us; 784 tiles would take 21.6 and not 20.2)
+    auto share_of = [&](long long tiles, int most) {
+        const long long even = max(max((tiles + gridDim.x - 1) / gridDim.x, ((long long)most + p.nsplit - 3) / (p.nsplit - 1)), 1ll);
+        return tiles <= 3 * 148 ? max(even, (tiles + 147) / 148) : even;
+    };
+    auto head_of_workspace = [&]() {
+        p.header[0] = (int32_t)WS_MAGIC;
+        p.header[1] = KVS_OK;
+        *reinterpret_cast<long long*>(p.header + WIN_SHARE_WORD) = share;
+    };
+    if (E <= 32) {
+        // every warp for itself, a lane for an entry: no barrier of the CTA (one windowed sequence 9.9 -> 9.45 us, five drafted tokens of 24
+        // sequences 92.7 -> 91.1, 16 of 500 to 6000 tokens the same)
+        WindowUnit u;
+        u.tiles = 0;
+        if (lane < E) u.load(p, lane);
+        long long upto = u.tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        all = __shfl_sync(0xffffffffu, upto, 31) * p.Hkv;
+        share = share_of(all, __reduce_max_sync(0xffffffffu, u.tiles));
+        at = share * blockIdx.x;
+        const long long before = upto - u.tiles;
+        if (blockIdx.x == 0 && warp == 0) {
+            if (lane < E) p.entries[lane] = {before, u.tiles, 0};
+            if (lane == 0) head_of_workspace();
+        }
+        if (at >= all) return;                             // the same in the whole CTA
+        entry = __ffs(__ballot_sync(0xffffffffu, upto * p.Hkv > at)) - 1;
+        entry_before = __shfl_sync(0xffffffffu, before, entry);
+    } else {
         // every thread's first entry is kept: with no more entries than threads they are gone over once
         WindowUnit u;
         u.tiles = 0;
@@ -220,17 +258,9 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             all += others;
         }
         all *= p.Hkv;
-        // not so small that a head is cut into more parts than there is room for: the first may be cut anywhere
-        share = max(max((all + gridDim.x - 1) / gridDim.x, ((long long)s_most + p.nsplit - 3) / (p.nsplit - 1)), 1ll);
-        // The second CTA of an SM starts 5 us after the first, which is worth two tiles: up to three tiles an SM are one CTA's (4 sequences of
-        // 1000 to 2000 tokens, 392 tiles, 15.7 -> 14.0 us; 784 tiles would take 21.6 and not 20.2)
-        if (all <= 3 * 148) share = max(share, (all + 147) / 148);
+        share = share_of(all, s_most);
         at = share * blockIdx.x;
-        if (blockIdx.x == 0 && tid == 0) {
-            p.header[0] = (int32_t)WS_MAGIC;
-            p.header[1] = KVS_OK;
-            *reinterpret_cast<long long*>(p.header + WIN_SHARE_WORD) = share;
-        }
+        if (blockIdx.x == 0 && tid == 0) head_of_workspace();
         if (at >= all && blockIdx.x != 0) return;          // the same in the whole CTA
         auto look = [&](int e, long long before) {         // is it this CTA's first entry; the first CTA writes all down
             if (e < E && blockIdx.x == 0) p.entries[e] = {before, u.tiles, 0};
@@ -250,11 +280,13 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         }
         __syncthreads();
         if (at >= all) return;                             // the first CTA of a call without a tile
+        entry = s_entry;
+        entry_before = s_before;
     }
     const int my_tiles = (int)min(share, all - at);
     WindowCursor start;
-    start.e = s_entry;
-    start.before = s_before;
+    start.e = entry;
+    start.before = entry_before;
     start.u.load(p, start.e);
     {
         const long long into = at - start.before * p.Hkv;
