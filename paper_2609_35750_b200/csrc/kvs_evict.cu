@@ -553,7 +553,8 @@ extern "C" int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recen
     const size_t alone = (size_t)((max_pages + 2) * page_bytes);
     if (num_seqs <= EV_MOST_CTAS && max_pages <= 2048 && alone <= EV_PLAIN_SMEM)
         return launch_clusters_after(evict_kernel<true>, dim3((unsigned)num_seqs), num_seqs, EV_THREADS, alone, st, p, max_pages);
-    if (smem > EV_PLAIN_SMEM && cudaFuncSetAttribute(evict_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    // the same limit in every call: it belongs to the function, and another thread's call may come between this line and the launch
+    if (smem > EV_PLAIN_SMEM && cudaFuncSetAttribute(evict_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_MOST_SMEM) != cudaSuccess)
         return cuda_refused();
     const int rc = launch_after(evict_plan_kernel, 1, plan_threads(num_seqs, false), 0, st, p);
     if (rc != KVS_OK) return rc;
