@@ -21,6 +21,7 @@ namespace cg = cooperative_groups;
 
 constexpr int VER_THREADS = 256;
 constexpr int VER_TILE = 256;               // tokens a warp adds up at a time: 8 loads of either row in flight a lane (512: 4 x 32000 6.6 -> 7.7 us; 1024: 128 x 131071 27 -> 42)
+constexpr int VER_MOST_SMEM = 64 * 1024;    // sums of 2^21 tokens' tiles: one CTA's part up to there, beyond that of eight CTAs
 
 struct VerifyParams {
     const float* target;        // [S, n + 1, V]
@@ -201,7 +202,8 @@ extern "C" int kvs_verify_drafts(const float* target_probs, const float* draft_p
     if (vocab > (1 << 21)) C = 8;                // the tiles' sums fit into shared memory
     VerifyParams p = {target_probs, draft_probs, draft_tokens, u_accept, u_sample, tokens, n_accepted, n_draft, vocab, (tiles + C - 1) / C * VER_TILE};
     const size_t smem = (size_t)(p.part / VER_TILE) * sizeof(double);
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(verify_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    // the same limit in every call: it belongs to the function, and another thread's call may come between this line and the launch
+    if (smem > 40 * 1024 && cudaFuncSetAttribute(verify_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, VER_MOST_SMEM) != cudaSuccess)
         return cuda_refused();
     return launch_clusters_after(verify_kernel, dim3((unsigned)(num_seqs * C)), C, VER_THREADS, smem, (cudaStream_t)stream, p);
 }

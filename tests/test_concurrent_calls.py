@@ -58,3 +58,21 @@ def test_evictions_of_caches_of_different_sizes():
         return work
 
     together(cache(32768, 30000, 300), cache(130000, 120000, 1000))
+
+
+def test_verifications_of_vocabularies_of_different_sizes():
+    def vocabulary(V):
+        g = torch.Generator(device="cuda").manual_seed(V)
+        p = torch.rand((1, 1, V), generator=g, device="cuda")
+        none = torch.zeros((1, 0), device="cuda")
+        u = torch.rand(1, generator=g, device="cuda")
+        once = lambda: B.kvs_verify_drafts(p, none.view(1, 0, 1).expand(1, 0, V).contiguous(), none.int(), none, u)  # noqa: E731
+        want = once()
+
+        def work():
+            got = [once() for _ in range(200)]
+            for one in got:
+                assert all(torch.equal(x, y) for x, y in zip(one, want))
+        return work
+
+    together(vocabulary(11_000_000), vocabulary(1 << 24))
