@@ -968,11 +968,12 @@ extern "C" int kvs_cache_evict(const int32_t* ranges, int n_ranges, int num_seqs
     if (!block_table || !n_tokens || !free_list || n_ranges < 0 || num_seqs < 0 || page_size <= 0 || max_pages <= 0 || num_pages <= 0)
         return KVS_ERR_INVALID_ARG;
     if (n_ranges > 0 && !ranges) return KVS_ERR_INVALID_ARG;
-    if ((size_t)max_pages * sizeof(int32_t) > 200 * 1024) return KVS_ERR_UNSUPPORTED;
-    if (n_ranges == 0 || num_seqs == 0) return KVS_OK;
+    constexpr size_t MOST_SMEM = 200 * 1024;
     const size_t smem = (size_t)max_pages * sizeof(int32_t);
-    if (smem > 48 * 1024 &&
-        cudaFuncSetAttribute(cache_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    if (smem > MOST_SMEM) return KVS_ERR_UNSUPPORTED;
+    if (n_ranges == 0 || num_seqs == 0) return KVS_OK;
+    // the same limit in every call: it belongs to the function, and another thread's call may come between this line and the launch
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(cache_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST_SMEM) != cudaSuccess)
         return cuda_refused();
     return launch_after(cache_evict_kernel, num_seqs, 256, smem, (cudaStream_t)stream, ranges, n_ranges, num_seqs, page_size, max_pages,
                         num_pages, block_table, n_tokens, free_list);

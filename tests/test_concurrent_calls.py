@@ -76,3 +76,23 @@ def test_verifications_of_vocabularies_of_different_sizes():
         return work
 
     together(vocabulary(11_000_000), vocabulary(1 << 24))
+
+
+def test_evictions_by_ranges_of_tables_of_different_sizes():
+    def cache(pages, calls=6000):
+        one = B.PagedCache.__new__(B.PagedCache)
+        free = torch.zeros(4 + pages, dtype=torch.int32, device="cuda")
+        one.__dict__.update(num_pages=pages, page_size=1, num_seqs=1, max_pages=pages, token_weight=None, free_list=free,
+                            block_table=torch.arange(pages, dtype=torch.int32, device="cuda").view(1, -1),
+                            n_tokens=torch.tensor([pages], dtype=torch.int32, device="cuda"))
+        ranges = torch.tensor([[0, 100, 1]], dtype=torch.int32, device="cuda")
+
+        def work():
+            stream = torch.cuda.current_stream()
+            for _ in range(calls):                                # page after page leaves from slot 100
+                one.evict(ranges, stream=stream)
+            assert int(one.n_tokens) == pages - calls and free[:2].tolist() == [calls, B.KVS_OK]
+            assert torch.equal(free[4:4 + calls].cpu(), torch.arange(100, 100 + calls, dtype=torch.int32))
+        return work
+
+    together(cache(13000), cache(51200))
