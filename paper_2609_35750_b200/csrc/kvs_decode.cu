@@ -38,7 +38,8 @@ struct DecodeParams {
     float* part_o;                   // [S, Hq, nsplit, D] unnormalised
     float* part_ml;                  // [S, Hq, nsplit, 2]  (max in base-2 units, sum; see flagged_sum)
     float* scores;                   // kvs_decode_attn_weights: [S, Hq, score_stride] scores in base-2 units of the live tokens
-    int score_stride;                // most tokens of a sequence, in whole tiles
+    int score_stride;                // most_scored in whole tiles
+    int most_scored;                 // tokens of a sequence that the caller said there are at most
 };
 
 __device__ __forceinline__ void decode_header(const DecodeParams& p) {
@@ -67,7 +68,7 @@ struct WeightParams {
     const float* scores;
     const int32_t* n_tokens;
     float* weight;                   // [S, weight_stride]
-    int Hq, score_stride, merge_ctas, chunks, steps;
+    int Hq, score_stride, most_scored, merge_ctas, chunks, steps;
     int weight_stride;               // max_pages * page_size: no sequence has more tokens
 };
 template <int D, int PART>
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(256, 4) decode_merge_weights_kernel(MergeParam
     }
     const int s = (blockIdx.x - w.merge_ctas) / w.chunks, j_first = (blockIdx.x - w.merge_ctas - s * w.chunks) * WT_TOKENS * w.steps;
     const int n = min(max(w.n_tokens[s], 0), w.weight_stride);
-    if (n > w.score_stride || j_first >= n) return;       // the same in the whole CTA
+    if (n > w.most_scored || j_first >= n) return;        // the same in the whole CTA
     // lse of the sequence's heads, a warp for a head
     const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + (size_t)s * w.Hq * p.nsplit;
     for (int h0 = warp; h0 < w.Hq; h0 += 32) {
@@ -172,9 +173,9 @@ __device__ __forceinline__ int checked_page(const DecodeParams& p, int page) {
     return 0;
 }
 
-// Tokens whose scores are written: all, or none of a sequence that is longer than the caller said (there is no room for them)
+// Tokens whose scores are written: all, or none of a sequence that is longer than the caller said (there need be no room for them)
 __device__ __forceinline__ int scored_tokens(const DecodeParams& p, int n) {
-    if (n <= p.score_stride) return n;
+    if (n <= p.most_scored) return n;
     set_status(p.status, KVS_ERR_INVALID_ARG);
     return 0;
 }
@@ -1084,13 +1085,13 @@ static int launch_decode(const DecodeParams& p, int G, const void* k_cache, cons
     const MergeParams m = {p.part_o, p.part_ml, out, lse, p.header, p.S * p.Hq, p.nsplit};
     const int merge_ctas = (m.rows + 7) / 8;
     if (!weight) return launch_after(p.nsplit <= 4 ? decode_merge_kernel<D, 4> : decode_merge_kernel<D, 16>, merge_ctas, 256, 0, st, m);
-    const int most = min(p.score_stride, p.max_pages * p.page_size);
+    const int most = min(p.most_scored, p.max_pages * p.page_size);
     // longer runs of tokens where CTAs come in several waves: each forms the lse once (48 caches of up to 16000 tokens, 1 to 8 steps chosen by
     // 3, 6, 12 and 24 CTAs an SM: 289, 283, 283, 286 us)
     int steps = 1;
     while (steps < 8 && (long long)p.S * ((most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps)) > 148 * 6) steps *= 2;
     const int chunks = (most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps);
-    const WeightParams w = {p.scores, p.n_tokens, weight, p.Hq, p.score_stride, merge_ctas, chunks, steps, p.max_pages * p.page_size};
+    const WeightParams w = {p.scores, p.n_tokens, weight, p.Hq, p.score_stride, p.most_scored, merge_ctas, chunks, steps, p.max_pages * p.page_size};
     if ((long long)merge_ctas + (long long)p.S * chunks > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
     return launch_after(p.nsplit <= 4 ? decode_merge_weights_kernel<D, 4> : decode_merge_weights_kernel<D, 8>, merge_ctas + p.S * chunks, 256,
                         sizeof(float) * (size_t)p.Hq, st, m, w);
@@ -1155,6 +1156,7 @@ static int decode_call(const void* q, const void* k_cache, const void* v_cache, 
     p.part_ml = p.part_o + (size_t)num_seqs * Hq * num_splits * head_dim;
     p.scores = token_weight ? (float*)((char*)workspace + plain) : nullptr;
     p.score_stride = token_weight ? (int)align_up((size_t)max_tokens, 128) : 0;
+    p.most_scored = max_tokens;
     cudaStream_t st = (cudaStream_t)stream;
     return head_dim == 64 ? launch_decode<64>(p, Hq / Hkv, k_cache, v_cache, (__nv_bfloat16*)out, lse, token_weight, st)
                           : launch_decode<128>(p, Hq / Hkv, k_cache, v_cache, (__nv_bfloat16*)out, lse, token_weight, st);
