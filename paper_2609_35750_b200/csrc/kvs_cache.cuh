@@ -114,6 +114,10 @@ __device__ __forceinline__ void decode_merge_row(const MergeParams& p, size_t ro
         *reinterpret_cast<uint32_t*>(p.out + row * D + lane * PER) = pack_bf16(acc[0], acc[1]);
     if (lane == 0) p.lse[row] = (L > 0.f) ? M * 0.6931471805599453f + logf(L) : -INFINITY;
 }
+// The row of this warp where CTAs of MERGE_WARPS warps have a row a warp.  There are up to 2^31 - 1 rows: their threads would not fit into 32 bits.
+constexpr int MERGE_WARPS = 8;
+__device__ __forceinline__ unsigned merge_row() { return blockIdx.x * (unsigned)MERGE_WARPS + (threadIdx.x >> 5); }
+inline unsigned merge_ctas(int rows) { return ((unsigned)rows + MERGE_WARPS - 1) / MERGE_WARPS; }
 // TMA gather: the 64-column slice starting at column c0 of the four rows r0..r3 of a 2-D tensor lands in four
 // consecutive 128-byte rows at dst (swizzled by address like a tiled box); completes 512 bytes on the barrier.
 __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, int c0, int r0, int r1, int r2, int r3, uint32_t bar) {

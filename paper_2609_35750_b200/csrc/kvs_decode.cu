@@ -50,10 +50,10 @@ __device__ __forceinline__ void decode_header(const DecodeParams& p) {
 }
 
 template <int D, int PART>
-__global__ void __launch_bounds__(256) decode_merge_kernel(MergeParams p) {
+__global__ void __launch_bounds__(32 * MERGE_WARPS) decode_merge_kernel(MergeParams p) {
     pdl_wait();
-    const int row = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    if (row < p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31, p.nsplit);
+    const unsigned row = merge_row();
+    if (row < (unsigned)p.rows) decode_merge_row<D, PART>(p, row, threadIdx.x & 31, p.nsplit);
 }
 
 // kvs_decode_attn_weights: token_weight[s, j] += sum over query heads of exp2(score - lse), in a fixed order of the heads, so that the
@@ -72,14 +72,14 @@ struct WeightParams {
     int weight_stride;               // max_pages * page_size: no sequence has more tokens
 };
 template <int D, int PART>
-__global__ void __launch_bounds__(256, 4) decode_merge_weights_kernel(MergeParams p, WeightParams w) {
+__global__ void __launch_bounds__(32 * MERGE_WARPS, 4) decode_merge_weights_kernel(MergeParams p, WeightParams w) {
     __shared__ float s_sum[8][WT_TOKENS];
     extern __shared__ float s_lse[];                      // [Hq] in base-2 units
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x < w.merge_ctas) {
-        const int row = blockIdx.x * 8 + warp;
-        if (row < p.rows) decode_merge_row<D, PART>(p, row, lane, p.nsplit);
+        const unsigned row = merge_row();
+        if (row < (unsigned)p.rows) decode_merge_row<D, PART>(p, row, lane, p.nsplit);
         return;
     }
     const int s = (blockIdx.x - w.merge_ctas) / w.chunks, j_first = (blockIdx.x - w.merge_ctas - s * w.chunks) * WT_TOKENS * w.steps;
@@ -1083,17 +1083,17 @@ static int launch_decode(const DecodeParams& p, int G, const void* k_cache, cons
     const int rc = weight ? launch_partials<D, true>(p, G, k_cache, v_cache, st) : launch_partials<D, false>(p, G, k_cache, v_cache, st);
     if (rc != KVS_OK) return rc;
     const MergeParams m = {p.part_o, p.part_ml, out, lse, p.header, p.S * p.Hq, p.nsplit};
-    const int merge_ctas = (m.rows + 7) / 8;
-    if (!weight) return launch_after(p.nsplit <= 4 ? decode_merge_kernel<D, 4> : decode_merge_kernel<D, 16>, merge_ctas, 256, 0, st, m);
+    const unsigned rows_ctas = merge_ctas(m.rows);
+    if (!weight) return launch_after(p.nsplit <= 4 ? decode_merge_kernel<D, 4> : decode_merge_kernel<D, 16>, rows_ctas, 32 * MERGE_WARPS, 0, st, m);
     const int most = min(p.most_scored, p.max_pages * p.page_size);
     // longer runs of tokens where CTAs come in several waves: each forms the lse once (48 caches of up to 16000 tokens, 1 to 8 steps chosen by
     // 3, 6, 12 and 24 CTAs an SM: 289, 283, 283, 286 us)
     int steps = 1;
     while (steps < 8 && (long long)p.S * ((most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps)) > 148 * 6) steps *= 2;
     const int chunks = (most + WT_TOKENS * steps - 1) / (WT_TOKENS * steps);
-    const WeightParams w = {p.scores, p.n_tokens, weight, p.Hq, p.score_stride, p.most_scored, merge_ctas, chunks, steps, p.max_pages * p.page_size};
-    if ((long long)merge_ctas + (long long)p.S * chunks > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
-    return launch_after(p.nsplit <= 4 ? decode_merge_weights_kernel<D, 4> : decode_merge_weights_kernel<D, 8>, merge_ctas + p.S * chunks, 256,
+    const WeightParams w = {p.scores, p.n_tokens, weight, p.Hq, p.score_stride, p.most_scored, (int)rows_ctas, chunks, steps, p.max_pages * p.page_size};
+    if ((long long)rows_ctas + (long long)p.S * chunks > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
+    return launch_after(p.nsplit <= 4 ? decode_merge_weights_kernel<D, 4> : decode_merge_weights_kernel<D, 8>, rows_ctas + p.S * chunks, 32 * MERGE_WARPS,
                         sizeof(float) * (size_t)p.Hq, st, m, w);
 }
 

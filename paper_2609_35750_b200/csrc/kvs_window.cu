@@ -762,11 +762,12 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
 // A warp for a row (sequence, token, query head): its head's tiles were `count` CTAs' work.  Loads of 8 parts at a time and three CTAs an SM
 // (16 and two: 24 sequences with 5 new tokens of 28 heads 95.6 -> 93.3 us, a round of 16 with 32 heads 62.1 -> 59.9).
 template <int D, int PART>
-__global__ void __launch_bounds__(256, 3) window_merge_kernel(MergeParams m, const WindowEntry* entries, int Hq, int G, int Hkv, int n_new, int groups,
+__global__ void __launch_bounds__(32 * MERGE_WARPS, 3) window_merge_kernel(MergeParams m, const WindowEntry* entries, int Hq, int G, int Hkv, int n_new, int groups,
                                                           int group_tokens) {
     pdl_wait();
-    const int row = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    if (row >= m.rows) return;
+    const unsigned at_row = merge_row();
+    if (at_row >= (unsigned)m.rows) return;
+    const int row = (int)at_row;
     const int token = row / Hq, g = (row - token * Hq) / G, s = token / n_new;
     const WindowEntry e = entries[s * groups + (token - s * n_new) / group_tokens];
     const long long share = *reinterpret_cast<const long long*>(m.header + WIN_SHARE_WORD), at = e.before * Hkv + (long long)g * e.tiles;
@@ -811,7 +812,7 @@ int launch_window_cols(const CUtensorMap& tk, const CUtensorMap& tv, const Windo
                  : cols <= 32 ? launch_window<D, 32>(tk, tv, p, most_tiles, pages, st)
                               : launch_window<D, 64>(tk, tv, p, most_tiles, pages, st);
     if (rc != KVS_OK) return rc;
-    return launch_after(p.nsplit <= 4 ? window_merge_kernel<D, 4> : window_merge_kernel<D, 8>, (unsigned)((m.rows + 7) / 8), 256, 0, st, m, p.entries, p.Hq,
+    return launch_after(p.nsplit <= 4 ? window_merge_kernel<D, 4> : window_merge_kernel<D, 8>, merge_ctas(m.rows), 32 * MERGE_WARPS, 0, st, m, p.entries, p.Hq,
                         p.G, p.Hkv, p.n_new, p.groups, p.group_tokens);
 }
 // rows' results, room for one part more than num_splits (a border may fall anywhere in a head's tiles); then the entries
