@@ -32,6 +32,7 @@
 // A tile in which some query does not see some key is masked by element.  V rows that no query sees are cleared in shared memory
 // (0 x NaN is NaN).  A V row that some see and others do not (the new tokens, the window's edge) may hold an infinity or a NaN: it is
 // cleared too and added by hand for the queries that see it (`patch`).
+#include <cfloat>
 #include <cstring>
 
 #include "kvs_cache.cuh"
@@ -40,7 +41,7 @@ namespace kvs {
 
 constexpr int WIN_PAGES = 1;         // one TMA box per page
 constexpr int WIN_ROWS = 2;          // K: TMA gather4; V: cp.async rows
-constexpr float WIN_UNSET = -1e30f;  // reference of a column that has seen no key yet: any score is far above it
+constexpr float WIN_UNSET = -FLT_MAX;  // reference of a column that has seen no key yet: any score is far above it, and a hidden key's -inf below it
 constexpr float WIN_NEAR = 30.f;     // weights of up to 2^30, sums and products of up to 2^30 x keys x |v|: far from what fp32 holds
 
 struct WindowEntry {                 // of the workspace, written by the first CTA
