@@ -26,8 +26,9 @@
 //
 // The softmax needs no maximum in most tiles: weights are taken against a reference per column in shared memory, which may lie anywhere
 // near the scores, because bf16 has the exponents of fp32 and a weight's 8 bits are the same at any size.  A tile goes on with it while no
-// score is more than 30 (in base-2 units) above, and a head begins with 0 where all scores of its first tile lie within 30 of that: one
-// barrier that also takes a vote.  Only else the columns' maxima are formed, the reference moves and O^T is rescaled.
+// score is more than 8 (in base-2 units) above, and a head begins with 7 where all scores of its first tile lie within 15 of 0: one
+// barrier that also takes a vote.  Only else the columns' maxima are formed, the reference moves to 7 above them and O^T is rescaled.  So
+// weights are at most 2^8, as in kvs_decode_attn (V may be as large), and a column's largest at least 2^-22 (products with V of 2^-104 still count).
 //
 // A tile in which some query does not see some key is masked by element.  V rows that no query sees are cleared in shared memory
 // (0 x NaN is NaN).  A V row that some see and others do not (the new tokens, the window's edge) may hold an infinity or a NaN: it is
@@ -42,7 +43,8 @@ namespace kvs {
 constexpr int WIN_PAGES = 1;         // one TMA box per page
 constexpr int WIN_ROWS = 2;          // K: TMA gather4; V: cp.async rows
 constexpr float WIN_UNSET = -FLT_MAX;  // reference of a column that has seen no key yet: any score is far above it, and a hidden key's -inf below it
-constexpr float WIN_NEAR = 30.f;     // weights of up to 2^30, sums and products of up to 2^30 x keys x |v|: far from what fp32 holds
+constexpr float WIN_OVER = 8.f;      // a score may be that much above its column's reference: weights of up to 2^8, sums of up to 2^8 x keys x |v|
+constexpr float WIN_AHEAD = 7.f;     // a reference is set that much above the scores it is set for, so that it need not move for the next larger one
 
 struct WindowEntry {                 // of the workspace, written by the first CTA
     long long before;                // tiles of the entries before it, for one KV head
@@ -335,7 +337,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         tmem_alloc(smem_u32(s_tmem), 4 * COLS);            // S^T twice and O^T, in a power of two
         tmem_relinquish();
     } else if (tid < COLS) {
-        s_ref[tid] = 0.f;
+        s_ref[tid] = WIN_AHEAD;
     }
     tc_fence_before();
     __syncthreads();
@@ -601,7 +603,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     float sc[CH], ref[CH];
                     scores(col0 + c0, sc, ref);
 #pragma unroll
-                    for (int x = 0; x < CH; ++x) above |= first ? !(fabsf(sc[x]) <= WIN_NEAR) : sc[x] - ref[x] > WIN_NEAR;
+                    for (int x = 0; x < CH; ++x) above |= first ? !(fabsf(sc[x]) <= WIN_AHEAD + WIN_OVER) : sc[x] - ref[x] > WIN_OVER;
                 }
             // the same decision in every thread.  In a head's first tile every column has to have seen a key: masked ones are looked at
             const bool grow = group_any(1, WORKERS, above || (first && masked));
@@ -631,7 +633,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     const float top = fmaxf(fmaxf(s_wmax[tid], s_wmax[COLS + tid]), fmaxf(s_wmax[2 * COLS + tid], s_wmax[3 * COLS + tid]));
                     const float ref = s_ref[tid];
                     float to = ref;
-                    if (tid < cols) to = first ? (top > -INFINITY ? top : WIN_UNSET) : top - ref > WIN_NEAR ? top : ref;
+                    if (tid < cols) to = first ? (top > -INFINITY ? top + WIN_AHEAD : WIN_UNSET) : top - ref > WIN_OVER ? top + WIN_AHEAD : ref;
                     s_alpha[tid] = first ? 1.f : fast_exp2(ref - to);        // nothing has been added up before the first
                     s_ref[tid] = to;
                 }
@@ -745,7 +747,7 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 ml[1] = flagged_sum(s_wmax[tid] + s_wmax[COLS + tid] + s_wmax[2 * COLS + tid] + s_wmax[3 * COLS + tid], *(volatile int32_t*)status);
             }
             if (left > 0) {
-                if (tid < COLS) s_ref[tid] = 0.f;
+                if (tid < COLS) s_ref[tid] = WIN_AHEAD;
 #pragma unroll
                 for (int x = 0; x < WIDE; ++x) l_part[x] = 0.f;
                 named_bar_sync(1, WORKERS);                         // the references are read by all
