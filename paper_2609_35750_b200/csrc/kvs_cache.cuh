@@ -105,14 +105,14 @@ __device__ __forceinline__ void decode_merge_row(const MergeParams& p, size_t ro
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const float inv = L == 0.f ? 0.f : 1.f / L;           // a NaN among the scores stays in both results
 #pragma unroll
     for (int e = 0; e < PER; ++e) acc[e] *= inv;
     if constexpr (PER == 4)
         *reinterpret_cast<uint2*>(p.out + row * D + lane * PER) = make_uint2(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]));
     else
         *reinterpret_cast<uint32_t*>(p.out + row * D + lane * PER) = pack_bf16(acc[0], acc[1]);
-    if (lane == 0) p.lse[row] = (L > 0.f) ? M * 0.6931471805599453f + logf(L) : -INFINITY;
+    if (lane == 0) p.lse[row] = L == 0.f ? -INFINITY : M * 0.6931471805599453f + logf(L);
 }
 // The row of this warp where CTAs of MERGE_WARPS warps have a row a warp.  There are up to 2^31 - 1 rows: their threads would not fit into 32 bits.
 constexpr int MERGE_WARPS = 8;
