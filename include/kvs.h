@@ -455,7 +455,7 @@ int kvs_cache_evict_lowest(int budget, int keep_first, int keep_recent,
 /*
  * Appends n_new tokens (k_new, v_new: bf16 [num_seqs, n_new, Hkv, head_dim]) to every sequence whose `active` byte is non-zero
  * (active == NULL: all), in order.  All of them or none: where the free pages or a table do not suffice nothing changes and the cache
- * status is KVS_ERR_WORKSPACE (KVS_ERR_INVALID_ARG for lengths or a stack that make no sense).  Pages are taken in the order of the sequences.
+ * status is KVS_ERR_WORKSPACE (KVS_ERR_INVALID_ARG for lengths or a stack that make no sense, whatever else is short).  Pages are taken in the order of the sequences.
  */
 int kvs_cache_append_tokens(const void* k_new, const void* v_new, const uint8_t* active,
                             int num_seqs, int n_new, int Hkv, int head_dim, int page_size, int max_pages, int num_pages,

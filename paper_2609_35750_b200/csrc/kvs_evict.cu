@@ -310,15 +310,21 @@ struct JoinParams {
     __nv_bfloat16* v_cache;
 };
 
+// Why a call is not begun, whichever sequence is looked at first: a state that makes no sense comes before a want of room.
+__device__ __forceinline__ int join_refusal(const JoinParams& p, bool senseless, bool full, int top, int total) {
+    if (senseless || top < 0 || top > p.num_pages) return KVS_ERR_INVALID_ARG;
+    return full || total > top ? KVS_ERR_WORKSPACE : KVS_OK;
+}
+
 // One CTA: pages for the new tokens of all sequences, or of none.  The j-th page of the call comes from stack[top - 1 - j].
 __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
     __shared__ int s_warp[33];
-    __shared__ int s_no;
+    __shared__ bool s_senseless, s_full;                 // set by any thread, cleared by none
     __shared__ int s_n[PLAN_THREADS], s_at[PLAN_THREADS];
     CacheHeader* hdr = reinterpret_cast<CacheHeader*>(p.free_buf);
     const int32_t* stack = p.free_buf + 4;
     const int tid = threadIdx.x;
-    if (tid == 0) s_no = KVS_OK;
+    if (tid == 0) s_senseless = s_full = false;
     __syncthreads();
     pdl_wait();
     auto joins = [&](int s) { return s < p.S && (!p.active || p.active[s]); };
@@ -329,14 +335,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) join_plan_kernel(JoinParams p) {
         if (!joins(s)) continue;
         const int n = p.n_tokens[s];
         const long long room = (long long)p.max_pages * p.page_size;
-        if (n < 0 || n > room) s_no = KVS_ERR_INVALID_ARG;
-        else if (n > room - p.n_new) s_no = KVS_ERR_WORKSPACE;
+        if (n < 0 || n > room) s_senseless = true;
+        else if (n > room - p.n_new) s_full = true;
         else sum += needs(n);
     }
-    block_prefix(sum, s_warp, total);                    // its synchronisations order s_no too
-    int no = s_no;
-    if (no == KVS_OK && (top < 0 || top > p.num_pages)) no = KVS_ERR_INVALID_ARG;
-    if (no == KVS_OK && total > top) no = KVS_ERR_WORKSPACE;
+    block_prefix(sum, s_warp, total);                    // its synchronisations order the two words too
+    const int no = join_refusal(p, s_senseless, s_full, top, total);
     __syncthreads();
     if (tid == 0) {
         hdr->refused = no != KVS_OK;
@@ -371,7 +375,7 @@ constexpr int JOIN_CTAS = 8, JOIN_THREADS = 512, JOIN_SEQS = 128;
 template <typename T>
 __global__ void __launch_bounds__(JOIN_THREADS) join_together_kernel(JoinParams p) {
     __shared__ int s_warp[33];
-    __shared__ int s_no;
+    __shared__ bool s_senseless, s_full;                 // set by any thread, cleared by none
     __shared__ int s_n[JOIN_SEQS], s_at[JOIN_SEQS];
     cg::cluster_group cluster = cg::this_cluster();
     CacheHeader* hdr = reinterpret_cast<CacheHeader*>(p.free_buf);
@@ -379,7 +383,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_together_kernel(JoinParams 
     const int tid = threadIdx.x, c = (int)cluster.block_rank();
     constexpr int PER = sizeof(T) / sizeof(__nv_bfloat16);
     const int words = p.row / PER;
-    if (tid == 0) s_no = KVS_OK;
+    if (tid == 0) s_senseless = s_full = false;
     __syncthreads();
     pdl_wait();
     const int top = hdr->top;
@@ -388,16 +392,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_together_kernel(JoinParams 
         const bool in = tid < p.S && (!p.active || p.active[tid]);
         const int n = in ? p.n_tokens[tid] : 0;
         const long long room = (long long)p.max_pages * p.page_size;
-        if (n < 0 || n > room) s_no = KVS_ERR_INVALID_ARG;
-        else if (in && n > room - p.n_new) s_no = KVS_ERR_WORKSPACE;
+        if (n < 0 || n > room) s_senseless = true;
+        else if (in && n > room - p.n_new) s_full = true;
         else if (in) need = pages_of(n + p.n_new, p.page_size) - pages_of(n, p.page_size);
         s_n[tid] = in ? n : -1;
     }
     const int at = block_prefix(need, s_warp, total);
     if (tid < JOIN_SEQS) s_at[tid] = at;
-    int no = s_no;
-    if (no == KVS_OK && (top < 0 || top > p.num_pages)) no = KVS_ERR_INVALID_ARG;
-    if (no == KVS_OK && total > top) no = KVS_ERR_WORKSPACE;
+    const int no = join_refusal(p, s_senseless, s_full, top, total);
     cluster.sync();                                      // all have read: now it may be written (and the sums are in place)
     if (c == 0 && tid == 0) {
         hdr->refused = no != KVS_OK;
