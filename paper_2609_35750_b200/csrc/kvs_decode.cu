@@ -1066,12 +1066,14 @@ static int launch_partials(const DecodeParams& p, int G, const void* k_cache, co
         if (rc != KVS_OK) return rc;
     } else {
         int rc = KVS_ERR_UNSUPPORTED;
-        switch (G) {
-            case 1: rc = launch_after(decode_partial_kernel<D, 1, SCORES>, grid, DEC_THREADS, 0, st, p); break;
-            case 2: rc = launch_after(decode_partial_kernel<D, 2, SCORES>, grid, DEC_THREADS, 0, st, p); break;
-            case 4: rc = launch_after(decode_partial_kernel<D, 4, SCORES>, grid, DEC_THREADS, 0, st, p); break;
-            case 7: rc = launch_after(decode_partial_kernel<D, 7, SCORES>, grid, DEC_THREADS, 0, st, p); break;
-            case 8: rc = launch_after(decode_partial_kernel<D, 8, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+        if (G == 1) rc = launch_after(decode_partial_kernel<D, 1, SCORES>, grid, DEC_THREADS, 0, st, p);
+        if constexpr (D == 64) {                // wider groups of head_dim 128 went to the tensor cores
+            switch (G) {
+                case 2: rc = launch_after(decode_partial_kernel<D, 2, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+                case 4: rc = launch_after(decode_partial_kernel<D, 4, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+                case 7: rc = launch_after(decode_partial_kernel<D, 7, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+                case 8: rc = launch_after(decode_partial_kernel<D, 8, SCORES>, grid, DEC_THREADS, 0, st, p); break;
+            }
         }
         if (rc != KVS_OK) return rc;
     }
