@@ -1056,7 +1056,6 @@ static int launch_partials(const DecodeParams& p, int G, const void* k_cache, co
             if ((long long)p.num_pages * ps > 0x7fffffffLL) return KVS_ERR_UNSUPPORTED;
             if ((rc = make_tmap_rows(&tk, k_cache, p.num_pages * ps, p.Hkv * 128)) != KVS_OK) return rc;
             switch (G) {
-                case 1: rc = launch_decode_tc<1, DTC_ROWS, SCORES>(tk, tv, p, st); break;
                 case 2: rc = launch_decode_tc<2, DTC_ROWS, SCORES>(tk, tv, p, st); break;
                 case 4: rc = launch_decode_tc<4, DTC_ROWS, SCORES>(tk, tv, p, st); break;
                 case 7: rc = launch_decode_tc<7, DTC_ROWS, SCORES>(tk, tv, p, st); break;
