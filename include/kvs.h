@@ -423,7 +423,8 @@ int kvs_decode_attn_window(const void* q, const void* k_cache, const void* v_cac
  * exp(scale * q[s,h].k_j - lse[s,h]) for every live token j (fp32 [num_seqs, max_pages * page_size], in the order of the live
  * cache, as kvs_cache_evict_lowest takes it), the heads added in a fixed order.  max_tokens: no sequence has more live tokens; the workspace has
  * room for that many scores per query head.  A longer sequence gets its attention, keeps its weights, and sets KVS_ERR_INVALID_ARG in
- * the workspace's status word.  num_splits as in kvs_decode_attn; kvs_decode_weights_num_splits gives one that fills the GPU.  Hq <= 8192.  Everything else as in kvs_decode_attn.
+ * the workspace's status word.  num_splits as in kvs_decode_attn; kvs_decode_weights_num_splits gives one that fills the GPU.  Hq <= 8192.
+ * Everything else as in kvs_decode_attn, Hq/Hkv in {1,2,4,7,8} too.
  */
 int kvs_decode_weights_num_splits(int num_seqs, int Hkv, int max_tokens);
 size_t kvs_decode_weights_workspace_bytes(int num_seqs, int Hq, int head_dim, int num_splits, int max_tokens);

@@ -89,8 +89,10 @@ __device__ __forceinline__ uint32_t score_bits(float x) {
 }
 
 // TOGETHER: at most EV_MOST_CTAS sequences, each small enough for a CTA.  They are one cluster: every CTA reads all lengths and forms the
-// plan itself, and nothing is written before all have, so that one launch does what takes two otherwise (four caches of 5000 tokens in
-// pages of 16, with the copy of the state before it, 12.7 -> 9.1 us).
+// plan itself, and nothing is written before all have, so that one launch does what takes two otherwise.  Up to what fits into shared memory
+// without asking for more, and 2048 pages.  Both sides, by two launches -> by one (us, with 4.6 for the copy of the state before it): four
+// caches in pages of 16: 1000 tokens 15.4 -> 10.8, 6500 16.4 -> 12.3 (the border), 10000 16.4 -> 13.4, 20000 16.7 -> 17.0, 40000 18.1 -> 24.6; in
+// one-token pages: 1000 16.5 -> 10.8, 2000 16.4 -> 12.4 (the border), 4000 16.4 -> 16.4, 10000 18.5 -> 22.6; one cache or eight about the same.
 template <bool TOGETHER>
 __global__ void __launch_bounds__(EV_THREADS) evict_kernel(EvictParams p, int cap) {
     extern __shared__ __align__(16) uint8_t smem_raw[];

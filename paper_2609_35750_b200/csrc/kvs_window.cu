@@ -5,8 +5,8 @@
 // products run on the tensor core in the transposed form, so that a tile's 128 keys fill its 128 rows and the few queries its columns:
 //   S^T [128 keys x N] = K [128 x d] Q^T            A = K tile, B = Q: column c is query head c % G of token c / G
 //   O^T [d x N]       += V^T [d x 128 keys] P^T     A = V tile read MN-major, B = P^T  (d = 64: rows 64 .. 127 repeat rows 0 .. 63)
-// Four softmax warps (a thread has a key of S^T and a column d of O^T; from 17 columns on eight, which halve the columns), a warp that
-// issues the products, one that loads K and two that load V (by one control warp a tile took 5900 clocks, 1300 of them to issue its 16 TMA
+// Four softmax warps (a thread has a key of S^T and a column d of O^T; from 17 columns on eight, each with half of the 32 or 64 that the
+// kernel is compiled for: of 35 columns four warps have 32 and four 3), a warp that issues the products, one that loads K and two that load V (by one control warp a tile took 5900 clocks, 1300 of them to issue its 16 TMA
 // instructions for K, as many for V; rows of 256 bytes take seven).  S^T of tile t + 1 is formed while tile t is in work; with a single buffer K
 // of tile t + 2 is asked for as soon as that is complete, V of tile t + 1 as soon as the second product of tile t is, and two CTAs an SM
 // overlap what is left of the chain; up to 16 columns two or three buffers do that (see `STAGES`).
@@ -17,9 +17,12 @@
 // head are on their way while the last one's result is written.  Fixed number of CTAs a sequence -> equal shares (us): one sequence with a
 // window of 256 14.1 -> 10.4, 16 of 500 to 6000 tokens with 5 new ones (with append and truncate) 70 -> 66, 24 of 3000 to 16000 the same.
 //
-// 64 sequences, 32 heads on 8, window 4096: 1.06 GB in 170 us, 6.2 TB/s (0.95 of the measured copy rate); nothing hidden, 48 sequences of up
-// to 16000 tokens: 253 us, 0.99; 64 of 7000 one-token pages 152 us, 0.9.  With 35 columns (5 new tokens, 7 heads a KV head) 0.47 GB in 91 us,
-// 0.79: 10 us until the first tile is through (launch, lengths, queries, first maxima), 12 between the first and the last CTA's end.
+// Whole calls on caches that are not in L2: 64 sequences, 32 heads on 8, window 4096: 1.06 GB in 174 us, 6.1 TB/s (0.93 of the measured copy
+// rate; 171 where calls follow one another on the same caches); nothing hidden, 48 sequences of up to 16000 tokens: 261 us, 0.98; 64 of 7000
+// one-token pages, 28 heads on 4: 156 us, 0.9.  Heads of 64 have tiles of half the bytes and the same chain: 64 of 8000 to 16000 tokens, 16
+// heads on 4, 166 us, 0.72, by one-token pages 159.  With 35 columns (5 new tokens, 7 heads a KV head) 0.47 GB in 97 us, 0.73 (92 on the same
+// caches): 10 us until the first tile is through (launch, lengths, queries, first maxima), 12 between the first and the last CTA's end.
+// With more than 16 columns 80 registers a thread do not suffice: 80 to 188 bytes a thread are spilled, by 16 columns none.
 //
 // Rows reach shared memory as in kvs_decode_attn: pages of 8 to 128 tokens that tile 128 by one TMA box each, others by rows (K by
 // TMA gather4, V by cp.async).
@@ -216,8 +219,8 @@ decode_window_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         *reinterpret_cast<long long*>(p.header + WIN_SHARE_WORD) = share;
     };
     if (E <= 32) {
-        // every warp for itself, a lane for an entry: no barrier of the CTA (one windowed sequence 9.9 -> 9.45 us, five drafted tokens of 24
-        // sequences 92.7 -> 91.1, 16 of 500 to 6000 tokens the same)
+        // every warp for itself, a lane for an entry: no barrier of the CTA (calls that follow one another on the same caches: one windowed
+        // sequence 9.9 -> 9.45 us, five drafted tokens of 24 sequences 92.7 -> 91.1, 16 of 500 to 6000 tokens the same)
         WindowUnit u;
         u.tiles = 0;
         if (lane < E) u.load(p, lane);
