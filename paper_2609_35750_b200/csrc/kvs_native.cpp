@@ -6,6 +6,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <climits>
+
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -436,6 +438,17 @@ int small(int64_t n, const char* name) {
     return (int)n;
 }
 
+// a number that the C interface takes as an int: one that is wider would mean another one there
+int fits(PyObject* o, const char* name) {
+    PyObject* i = PyNumber_Index(o);
+    if (!i) throw Raised();
+    int wide = 0;
+    const long long v = PyLong_AsLongLongAndOverflow(i, &wide);
+    Py_DECREF(i);
+    if (wide || v < INT_MIN || v > INT_MAX) value_error("%s does not fit into 32 bits", name);
+    return (int)v;
+}
+
 // The cache that an attention call reads: sizes and addresses
 struct Cache {
     int64_t S, P, pages, page, Hkv, d;
@@ -463,10 +476,10 @@ PyObject* decode_window(PyObject* const* a) {
     const Cache c(a + 1, q);
     const int64_t new_ = q.size(1), Hq = q.size(2);
     const void* pq = checked(q, "q", BF16, {c.S, new_, Hq, c.d}, q);
-    const int window = whole(a[5]), sinks = whole(a[6]);
+    const int window = fits(a[5], "window"), sinks = fits(a[6], "sinks");
     const float scale = real(a[7]);
-    const int S = (int)c.S, n = small(new_, "q"), H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[12]), most = given_most ? given_most : (int)(c.P * c.page);
-    int splits = whole(a[8]);
+    const int S = (int)c.S, n = small(new_, "q"), H = small(Hq, "q"), d = (int)c.d, given_most = fits(a[12], "max_tokens"), most = given_most ? given_most : (int)(c.P * c.page);
+    int splits = fits(a[8], "num_splits");
     if (splits <= 0) splits = lib.kvs_decode_window_num_splits(S, n, H, (int)c.Hkv, most, window, sinks);
     const Scratch ws(a[11], lib.kvs_decode_window_workspace_bytes(S, n, H, (int)c.Hkv, d, splits), q);
     const at::Tensor out = out_of(a[9], "out", q), lse = out_of(a[10], "lse", {c.S, new_, Hq}, q, F32);
@@ -489,8 +502,8 @@ PyObject* decode_weights(PyObject* const* a) {
     const void* pq = checked(q, "q", BF16, {c.S, Hq, c.d}, q);
     float* pw = (float*)checked(w, "token_weight", F32, {c.S, c.P * c.page}, q);
     const float scale = real(a[6]);
-    const int S = (int)c.S, H = small(Hq, "q"), d = (int)c.d, given_most = whole(a[11]), most = given_most ? given_most : (int)(c.P * c.page);
-    int splits = whole(a[7]);
+    const int S = (int)c.S, H = small(Hq, "q"), d = (int)c.d, given_most = fits(a[11], "max_tokens"), most = given_most ? given_most : (int)(c.P * c.page);
+    int splits = fits(a[7], "num_splits");
     if (splits <= 0) splits = lib.kvs_decode_weights_num_splits(S, (int)c.Hkv, most);
     const Scratch ws(a[10], lib.kvs_decode_weights_workspace_bytes(S, H, d, splits, most), q);
     const at::Tensor out = out_of(a[8], "out", q), lse = out_of(a[9], "lse", {c.S, Hq}, q, F32);
@@ -527,7 +540,7 @@ PyObject* cache_append_tokens(PyObject* const* a) {
 
 // (n_drafted, n_accepted, page_size, block_table, n_tokens, free_list, token_weight, stream)
 PyObject* cache_truncate(PyObject* const* a) {
-    const int drafted = whole(a[0]), page = whole(a[2]);
+    const int drafted = fits(a[0], "n_drafted"), page = fits(a[2], "page_size");
     const at::Tensor &acc = tensor(a[1], "n_accepted"), &table = tensor(a[3], "block_table"), &n = tensor(a[4], "n_tokens"), &free = tensor(a[5], "free_list");
     dims(table, 2, "block_table");
     dims(free, 1, "free_list");
@@ -544,7 +557,7 @@ PyObject* cache_truncate(PyObject* const* a) {
 
 // (budget, keep_first, keep_recent, page_size, block_table, n_tokens, free_list, token_weight, evicted, n_evicted, stream)
 PyObject* cache_evict_lowest(PyObject* const* a) {
-    const int budget = whole(a[0]), first = whole(a[1]), recent = whole(a[2]), page = whole(a[3]);
+    const int budget = fits(a[0], "budget"), first = fits(a[1], "keep_first"), recent = fits(a[2], "keep_recent"), page = fits(a[3], "page_size");
     const at::Tensor &table = tensor(a[4], "block_table"), &n = tensor(a[5], "n_tokens"), &free = tensor(a[6], "free_list"), &w = tensor(a[7], "token_weight");
     dims(table, 2, "block_table");
     dims(free, 1, "free_list");
